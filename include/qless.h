@@ -9,6 +9,9 @@
  *                                 checkpoints, reduced by max over validation examples
  *   qless_topk      Sec. 4.1      selection of the highest-scoring training examples
  *   qless_aggregate Sec. 4.1      maximum / mean of the influences over groups of validation examples
+ * and, before them, what per-example gradients are made of:
+ *   qless_checkpoint8             activations kept in 8 bits from the forward to the backward pass
+ *   qless_checkpoint8_grad        per-example weight gradients from them, as rows to project
  *
  * Conventions common to every call
  *   - "device" pointers are HIP device memory owned by the caller; "host" pointers are ordinary
@@ -314,6 +317,46 @@ qless_status qless_score_groups(const void *const *train_codes, const float *con
                                 const float *eta, int C, int64_t N, int32_t M, int32_t k, int bits,
                                 const int32_t *group_end, int T, qless_agg mode, float *out,
                                 void *ws, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Activation checkpoints in 8 bits: a layer's input X (a row per token) is kept as codes and steps from the forward to
+ * the backward pass, half (bfloat16) or a quarter (fp32) of its size.  A group is QLESS_CHECKPOINT_GROUP columns of a row (the last
+ * one may be shorter), top its largest absolute value:
+ *   step  = the least number of eight significant bits, at least 2^-126, with 127 step >= top    (0 if top is 0)
+ *   code  = rne(X / step), the exact quotient rounded to the nearest whole number, ties to even; |code| <= 127
+ * so that X is read back as code * step (exact in fp32) to within step / 2.  A group that holds an infinity or a NaN is stored with
+ * the step NaN and codes 0: it reads back as NaN.
+ *   X      device, T x D, row-major with leading dimension ldX (elements) >= D, dtype dt
+ *   codes  device, T rows of D int8, leading dimension ldC >= D (bytes between a row's end and the next row are left as they are)
+ *   step   device, T rows of ceil(D / QLESS_CHECKPOINT_GROUP) fp32, leading dimension ldS
+ * qless_checkpoint8_read writes X = code * step, rounded once (to nearest even) for QLESS_BF16.  No alignment is required of
+ * rows beyond that of their elements.  T == 0 is valid; leading dimensions are not read where T <= 1.
+ * ------------------------------------------------------------------------------------------- */
+#define QLESS_CHECKPOINT_GROUP 128
+qless_status qless_checkpoint8(const void *X, qless_dtype dt, int64_t T, int32_t D, int64_t ldX, int8_t *codes, int64_t ldC,
+                               float *step, int64_t ldS, void *stream);
+qless_status qless_checkpoint8_read(const int8_t *codes, int64_t ldC, const float *step, int64_t ldS, int64_t T, int32_t D,
+                                    void *X, qless_dtype dt, int64_t ldX, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * The weight gradient of a linear layer Y = X A^T (A: R x D), one per example, from the layer's checkpointed input:
+ *   G_e[r][d] = sum over the tokens t of example e of dY[t][r] * code[t][d] * step[t][d / QLESS_CHECKPOINT_GROUP]
+ * Example e is the tokens [offsets[e], offsets[e + 1]); an empty one gets a gradient of zeros; tokens before offsets[0] and from
+ * offsets[n] on are not read.  Row e of G is the R x D matrix row by row, so that G may be a slice of the rows that
+ * qless_project and qless_project_quantize_slice read; n = 1 is the gradient of a whole batch.
+ *   dY       device, T x R, leading dimension ldY >= R, dtype dtY
+ *   codes, step   as written by qless_checkpoint8
+ *   offsets  device, n + 1 int64, not decreasing, within [0, T] (others give an unspecified G; nothing outside the operands
+ *            is touched);  n <= 65535
+ *   G        device, n rows of R * D, leading dimension ldG >= R * D (not read where n == 1), dtype dtG; what lies between the rows stays
+ *   ws       device workspace, 16-byte aligned, of at least qless_checkpoint8_grad_workspace(T, n, R, D) bytes
+ * Arithmetic: fp32 G: products of dY and step enter whole (dtY bfloat16) or to 2^-24 (fp32), products with codes are exact, sums are fp32.
+ * bfloat16 G: dY * step is rounded to bfloat16 once, sums are fp32 and rounded once.  Results are run-to-run identical.
+ * ------------------------------------------------------------------------------------------- */
+size_t qless_checkpoint8_grad_workspace(int64_t T, int64_t n, int32_t R, int32_t D);
+qless_status qless_checkpoint8_grad(const void *dY, qless_dtype dtY, int64_t ldY, int32_t R, const int8_t *codes, int64_t ldC,
+                                    const float *step, int64_t ldS, int32_t D, int64_t T, const int64_t *offsets, int64_t n,
+                                    void *G, qless_dtype dtG, int64_t ldG, void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

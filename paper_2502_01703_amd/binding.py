@@ -51,6 +51,11 @@ EXPORTS = {
     "qless_score_groups_workspace": (_sz, [_i64, _i32, _i32, _c.c_int, _c.c_int]),
     "qless_score_groups": (_c.c_int, [_vp, _vp, _vp, _vp, _vp, _c.c_int, _i64, _i32, _i32, _c.c_int, _vp, _c.c_int,
                                       _c.c_int, _vp, _vp, _sz, _vp]),
+    "qless_checkpoint8": (_c.c_int, [_vp, _c.c_int, _i64, _i32, _i64, _vp, _i64, _vp, _i64, _vp]),
+    "qless_checkpoint8_read": (_c.c_int, [_vp, _i64, _vp, _i64, _i64, _i32, _vp, _c.c_int, _i64, _vp]),
+    "qless_checkpoint8_grad_workspace": (_sz, [_i64, _i64, _i32, _i32]),
+    "qless_checkpoint8_grad": (_c.c_int, [_vp, _c.c_int, _i64, _i32, _vp, _i64, _vp, _i64, _i32, _i64, _vp, _i64, _vp, _c.c_int, _i64,
+                                          _vp, _sz, _vp]),
 }
 
 
@@ -102,7 +107,7 @@ def _dtype_code(t):
         return F32
     if t.dtype == torch.bfloat16:
         return BF16
-    raise TypeError("gradients must be float32 or bfloat16")
+    raise TypeError("tensors must be float32 or bfloat16")
 
 
 def _ws(nbytes, device):
@@ -379,3 +384,83 @@ def score_groups(train_codes, train_rnorm, val_codes, val_rnorm, eta, k, bits, g
                                     ge, T, mode, out.data_ptr(), w.data_ptr(), w.numel(),
                                     _stream()), "qless_score_groups")
     return out
+
+
+CHECKPOINT_GROUP = 128                  # QLESS_CHECKPOINT_GROUP of qless.h: columns that share a step
+
+
+def _rows(t, dtype=None):
+    """Checks a device matrix whose rows are dense, and returns its leading dimension."""
+    assert t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1) and (dtype is None or t.dtype == dtype)
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+
+
+class _On:
+    """The device of a call's tensors as the current one: kernels and workspaces belong there."""
+
+    def __init__(self, *tensors):
+        self.device = tensors[0].device
+        for t in tensors:
+            assert t is None or t.device == self.device, "all tensors of a call lie on one device"
+
+    def __enter__(self):
+        self.before = torch.cuda.current_device()
+        if self.device.index != self.before:
+            torch.cuda.set_device(self.device)
+
+    def __exit__(self, *_):
+        if self.device.index != self.before:
+            torch.cuda.set_device(self.before)
+
+
+def checkpoint8(X, codes=None, step=None):
+    """qless_checkpoint8: activations X [T, D] (fp32 or bf16, row stride free) -> (codes int8 [T, D],
+    step fp32 [T, ceil(D / 128)])."""
+    ldX = _rows(X)
+    T, D = X.shape
+    with _On(X, codes, step):
+        if codes is None:
+            codes = torch.empty(T, D, dtype=torch.int8, device=X.device)
+        if step is None:
+            step = torch.empty(T, -(-D // CHECKPOINT_GROUP), dtype=torch.float32, device=X.device)
+        assert codes.shape == X.shape and step.shape == (T, -(-D // CHECKPOINT_GROUP))
+        _check(lib().qless_checkpoint8(X.data_ptr(), _dtype_code(X), T, D, ldX, codes.data_ptr(), _rows(codes, torch.int8),
+                                       step.data_ptr(), _rows(step, torch.float32), _stream()), "qless_checkpoint8")
+    return codes, step
+
+
+def checkpoint8_read(codes, step, dtype=torch.bfloat16, out=None):
+    """qless_checkpoint8_read: codes [T, D] and steps -> the activations [T, D] in fp32 or bf16."""
+    ldC, ldS = _rows(codes, torch.int8), _rows(step, torch.float32)
+    T, D = codes.shape
+    assert step.shape == (T, -(-D // CHECKPOINT_GROUP))
+    with _On(codes, step, out):
+        if out is None:
+            out = torch.empty(T, D, dtype=dtype, device=codes.device)
+        assert out.shape == codes.shape
+        _check(lib().qless_checkpoint8_read(codes.data_ptr(), ldC, step.data_ptr(), ldS, T, D, out.data_ptr(), _dtype_code(out),
+                                            _rows(out), _stream()), "qless_checkpoint8_read")
+    return out
+
+
+def checkpoint8_grad_workspace(T, n, R, D):
+    return int(lib().qless_checkpoint8_grad_workspace(T, n, R, D))
+
+
+def checkpoint8_grad(dY, codes, step, offsets, dtype=torch.float32, out=None, ws=None):
+    """qless_checkpoint8_grad: dY [T, R] and a checkpointed input [T, D], examples [offsets[e], offsets[e + 1]) (device, int64) ->
+    G [n, R, D], or into `out` [n, R * D] (fp32 or bf16, row stride free: a slice of the rows to project)."""
+    ldY, ldC, ldS = _rows(dY), _rows(codes, torch.int8), _rows(step, torch.float32)
+    T, R = dY.shape
+    D = codes.shape[1]
+    n = offsets.numel() - 1
+    assert codes.shape[0] == T and step.shape == (T, -(-D // CHECKPOINT_GROUP))
+    assert offsets.is_cuda and offsets.dtype == torch.int64 and offsets.dim() == 1 and offsets.is_contiguous() and n >= 0
+    with _On(dY, codes, step, offsets, out, ws):
+        G = torch.empty(n, R * D, dtype=dtype, device=dY.device) if out is None else out
+        assert G.shape == (n, R * D)
+        w = _ws(checkpoint8_grad_workspace(T, n, R, D), dY.device) if ws is None else ws
+        _check(lib().qless_checkpoint8_grad(dY.data_ptr(), _dtype_code(dY), ldY, R, codes.data_ptr(), ldC, step.data_ptr(), ldS, D, T,
+                                            offsets.data_ptr(), n, G.data_ptr(), _dtype_code(G), _rows(G),
+                                            w.data_ptr(), w.numel(), _stream()), "qless_checkpoint8_grad")
+    return G.view(n, R, D) if out is None else G

@@ -1,0 +1,435 @@
+// qless_checkpoint8, qless_checkpoint8_read, qless_checkpoint8_grad: activations kept in 8 bits between the forward and the
+// backward pass, and the per-example weight gradients that are taken from them.
+//
+// A group is 128 columns of a row (the last one of a row may be shorter).  Its step s is the least number of eight significant
+// bits, at least 2^-126, of which 127 reach the group's largest absolute value; a code is the nearest whole number of steps, ties
+// to even, so that |code| <= 127.  Eight bits of step cost at most 1/128 of resolution, and buy products: a code (7 bits) is a
+// bfloat16, and a bfloat16 gradient times a step (16 bits) is the sum of two, so that the backward pass is exact up to its
+// fp32 sums with two matrix products instead of three.  A group with an infinity or a NaN gets the step NaN and codes 0.
+#include "common.h"
+
+namespace qless {
+
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) short i16x4;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+
+constexpr int kGroup = QLESS_CHECKPOINT_GROUP;
+
+__device__ inline float bf16_value(uint32_t bits) { return __uint_as_float(bits << 16); }
+__device__ inline uint16_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+
+// Eight elements from p on, whatever its alignment; those past `left` are 0 (left <= 0: none is read).
+template <class T> struct Eight;
+template <> struct Eight<float> {
+    static __device__ inline void load(const float *p, int64_t left, float (&x)[8]) {
+        if (left >= 8) __builtin_memcpy(x, p, 32);
+        else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = i < left ? p[i] : 0.0f;
+    }
+    static __device__ inline void store(float *p, int64_t left, const float (&x)[8]) {
+        if (left >= 8) __builtin_memcpy(p, x, 32);
+        else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) if (i < left) p[i] = x[i];
+    }
+};
+template <> struct Eight<uint16_t> {                      // bfloat16
+    static __device__ inline void load(const uint16_t *p, int64_t left, float (&x)[8]) {
+        uint16_t b[8];
+        if (left >= 8) __builtin_memcpy(b, p, 16);
+        else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) b[i] = i < left ? p[i] : (uint16_t)0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = bf16_value(b[i]);
+    }
+    static __device__ inline void store(uint16_t *p, int64_t left, const float (&x)[8]) {
+        uint16_t b[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] = bf16_bits(x[i]);
+        if (left >= 8) __builtin_memcpy(p, b, 16);
+        else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) if (i < left) p[i] = b[i];
+    }
+};
+
+// Maximum over the 16 lanes of a DPP row, in all of them.
+template <int CTRL> __device__ inline uint32_t row_rotate(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false);
+}
+__device__ inline uint32_t row_max(uint32_t x) {
+    x = max(x, row_rotate<0x128>(x)); x = max(x, row_rotate<0x124>(x));
+    x = max(x, row_rotate<0x122>(x)); x = max(x, row_rotate<0x121>(x));
+    return x;
+}
+
+// The step of a group whose largest absolute value has the bits `top` (order of non-negative floats; above: infinity, NaN).
+__device__ inline float group_step(uint32_t top) {
+    if (top == 0) return 0.0f;
+    if (top >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
+    const float a = __uint_as_float(top);
+    const float s = __uint_as_float((__float_as_uint(__fdiv_rn(a, 127.0f)) + 0xFFFFu) & 0xFFFF0000u);
+    // 127 s is exact (15 bits); the quotient may have been rounded down onto a number of eight bits
+    const float t = __fmul_rn(s, 127.0f) < a ? __uint_as_float(__float_as_uint(s) + 0x10000u) : s;
+    return fmaxf(t, 1.17549435e-38f);
+}
+// The nearest whole number of steps: the product with the rounded reciprocal is off by less than 2^-16, the remainder
+// x - q s is exact (q s has 15 bits, and no bit of x lies below 2^-25 s unless q is 0) and says on which side of the half x lies.
+__device__ inline int nearest_code(float x, float s, float inv) {
+    float q = rintf(__fmul_rn(x, inv));
+    const float r = __builtin_fmaf(-q, s, x), twice = fabsf(r + r);
+    const bool odd = ((int)q & 1) != 0;
+    if (twice > s || (twice == s && odd)) q += r < 0.0f ? -1.0f : 1.0f;
+    return (int)q;
+}
+
+// 16 lanes a group, eight columns a lane.  Bound: memory, read once and written once.
+template <class T>
+__global__ void __launch_bounds__(256)
+checkpoint_write_kernel(const T *X, int64_t rows, int32_t D, int64_t ldX, int32_t groups, int8_t *codes, int64_t ldC, float *step, int64_t ldS) {
+    const int64_t total = rows * groups, stride = (int64_t)gridDim.x * 16;
+    for (int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); i < total; i += stride) {
+        const int64_t t = i / groups;
+        const int g = (int)(i - t * groups), c = g * kGroup + (threadIdx.x & 15) * 8;
+        float x[8];
+        Eight<T>::load(X + t * ldX + c, D - c, x);
+        uint32_t top = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+        top = row_max(top);
+        const float s = group_step(top);
+        const bool plain = top != 0 && top < 0x7F800000u;
+        const float inv = plain ? __fdiv_rn(1.0f, s) : 0.0f;
+        int8_t q[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[j] = plain ? (int8_t)nearest_code(x[j], s, inv) : (int8_t)0;
+        int8_t *out = codes + t * ldC + c;
+        if (D - c >= 8) __builtin_memcpy(out, q, 8);
+        else
+#pragma unroll
+            for (int j = 0; j < 8; ++j) if (j < D - c) out[j] = q[j];
+        if ((threadIdx.x & 15) == 0) step[t * ldS + g] = s;
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(256)
+checkpoint_read_kernel(const int8_t *codes, int64_t ldC, const float *step, int64_t ldS, int64_t rows, int32_t D, int32_t groups, T *X, int64_t ldX) {
+    const int64_t total = rows * groups, stride = (int64_t)gridDim.x * 16;
+    for (int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); i < total; i += stride) {
+        const int64_t t = i / groups;
+        const int g = (int)(i - t * groups), c = g * kGroup + (threadIdx.x & 15) * 8, left = D - c;
+        const int8_t *in = codes + t * ldC + c;
+        int8_t q[8];
+        if (left >= 8) __builtin_memcpy(q, in, 8);
+        else
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q[j] = j < left ? in[j] : (int8_t)0;
+        const float s = step[t * ldS + g];
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = __fmul_rn((float)q[j], s);
+        Eight<T>::store(X + t * ldX + c, left, x);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------------
+// Weight gradients per example: G_e[r][d] = sum over the tokens t of example e of dY[t][r] code[t][d] step[t][d / 128].
+//
+// The tokens are cut at the multiples of `chunk` and at the examples' ends.  With phi(e) = e + floor(offset[e] / chunk), example e
+// owns the segments phi(e) .. phi(e + 1) - 1 (the last may be empty), which any workgroup finds by bisection, with no list of
+// them in memory; an example of one segment is written at once, the others' segments leave fp32 planes that a second kernel adds in
+// their order.
+struct GradArgs {
+    const void *dY; int64_t ldY;
+    const int8_t *codes; int64_t ldC;
+    const float *step; int64_t ldS;
+    const int64_t *offsets;
+    int64_t n, T, chunk, segments;
+    int32_t R, D, rtiles, dtiles;
+    void *G; int64_t ldG;
+    float *planes;                                         // [segments][R][D]
+};
+struct Segment { int64_t e, lo, hi; bool whole; };
+
+__device__ inline int64_t offset_at(const GradArgs &a, int64_t e) {      // never outside the tokens, whatever the caller wrote there
+    const int64_t o = a.offsets[e];
+    return o < 0 ? 0 : (o > a.T ? a.T : o);
+}
+__device__ inline int64_t phi(const GradArgs &a, int64_t e) { return e + offset_at(a, e) / a.chunk; }
+__device__ inline bool find_segment(const GradArgs &a, int64_t j, Segment &s) {
+    if (j < phi(a, 0) || j >= phi(a, a.n)) return false;
+    int64_t lo = 0, hi = a.n;                              // phi(lo) <= j < phi(hi)
+    while (hi - lo > 1) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (phi(a, mid) <= j) lo = mid; else hi = mid;
+    }
+    const int64_t o0 = offset_at(a, lo), o1 = offset_at(a, lo + 1), i = j - (lo + o0 / a.chunk);
+    const int64_t c0 = (o0 / a.chunk + i) * a.chunk, c1 = c0 + a.chunk;
+    s.e = lo;
+    s.lo = c0 > o0 ? c0 : o0;
+    s.hi = c1 < o1 ? c1 : o1;
+    s.whole = o0 / a.chunk == o1 / a.chunk;
+    return true;
+}
+
+// Tiles of RT rows of R x 128 columns (one group: a token has one step there), four wavefronts, 64 tokens a stage.  A stage's codes
+// become bfloat16, its gradients times their step the sum of TERMS bfloat16; both lie in LDS as rows of a token, and the matrix operands
+// (eight tokens of a column in a lane) are formed by the transposing LDS reads.  The order of the tokens inside a product is that of
+// those reads, alike on both sides.  32-byte pieces of a row are exchanged by its token's low bits: the eight rows that 32 lanes read
+// together lie in different banks.
+template <int RT, class Y, int TERMS, class Out>
+__global__ void __launch_bounds__(256)
+checkpoint_grad_kernel(GradArgs a) {
+    constexpr int KT = 64, WY = RT >= 64 ? 2 : 1, WX = 4 / WY, CM = 128 / WX / 16, CN = RT / WY / 16;
+    constexpr int YROW = RT * 2, YPLANE = KT * YROW, PIECES = KT * RT / 8, PER = (PIECES + 255) / 256;
+    __shared__ __attribute__((aligned(16))) unsigned char s_codes[KT * 256];
+    __shared__ __attribute__((aligned(16))) unsigned char s_y[TERMS * YPLANE];
+    const int64_t tiles = (int64_t)a.rtiles * a.dtiles, j = blockIdx.x / tiles;
+    const int tile = (int)(blockIdx.x - j * tiles), rt = tile / a.dtiles, g = tile - rt * a.dtiles;
+    Segment seg;
+    if (!find_segment(a, j, seg)) return;                  // the whole workgroup
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wy = wave / WX, wx = wave % WX;
+    const int r0 = rt * RT, d0 = g * kGroup, l16 = lane & 15, quad = lane >> 4;
+    auto yswizzle = [](int k) { return RT >= 128 ? k & 7 : RT == 64 ? (k >> 1) & 3 : RT == 32 ? (k >> 2) & 1 : 0; };
+
+    f32x4 acc[CM][CN];
+#pragma unroll
+    for (int m = 0; m < CM; ++m)
+#pragma unroll
+        for (int n = 0; n < CN; ++n) acc[m][n] = f32x4{0, 0, 0, 0};
+
+    float y[PER][8];
+    int8_t q[32];
+    auto request = [&](int64_t t0) {
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            const int piece = tid + 256 * p, k = piece / (RT / 8), r = r0 + piece % (RT / 8) * 8;
+            const int64_t t = t0 + k;
+            const bool live = piece < PIECES && t < seg.hi;
+            Eight<Y>::load((const Y *)a.dY + t * a.ldY + r, live ? a.R - r : 0, y[p]);
+            const float s = live ? a.step[t * a.ldS + g] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[p][i] = live ? __fmul_rn(y[p][i], s) : 0.0f;
+        }
+        const int64_t t = t0 + (tid >> 2);
+        const int c = d0 + (tid & 3) * 32, left = t < seg.hi ? a.D - c : 0;
+        const int8_t *in = a.codes + t * a.ldC + c;
+        if (left >= 32) __builtin_memcpy(q, in, 32);
+        else
+#pragma unroll
+            for (int i = 0; i < 32; ++i) q[i] = i < left ? in[i] : (int8_t)0;
+    };
+    auto store = [&]() {
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            const int piece = tid + 256 * p, k = piece / (RT / 8), c = piece % (RT / 8);
+            if (piece < PIECES) {
+#pragma unroll
+                for (int term = 0; term < TERMS; ++term) {
+                    uint16_t b[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        b[i] = bf16_bits(y[p][i]);
+                        y[p][i] = __fsub_rn(y[p][i], bf16_value(b[i]));       // exact
+                    }
+                    __builtin_memcpy(__builtin_assume_aligned(s_y + term * YPLANE + k * YROW + (((c >> 1) ^ yswizzle(k)) << 5) + ((c & 1) << 4), 16), b, 16);
+                }
+            }
+        }
+        const int k = tid >> 2;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            uint16_t b[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) b[i] = (uint16_t)(__float_as_uint((float)q[8 * h + i]) >> 16);
+            const int c = (tid & 3) * 4 + h;
+            __builtin_memcpy(__builtin_assume_aligned(s_codes + k * 256 + (((c >> 1) ^ (k & 7)) << 5) + ((c & 1) << 4), 16), b, 16);
+        }
+    };
+    typedef __attribute__((address_space(3))) i16x4 lds16x4;
+    auto column = [](const unsigned char *lo, const unsigned char *hi) {     // tokens of two times four rows
+        const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)lo);
+        const i16x4 z = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)hi);
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, z, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+
+    if (seg.lo < seg.hi) request(seg.lo);
+    for (int64_t t0 = seg.lo; t0 < seg.hi; t0 += KT) {
+        __syncthreads();
+        store();
+        __syncthreads();
+        if (t0 + KT < seg.hi) request(t0 + KT);
+#pragma unroll
+        for (int kk = 0; kk < KT / 32; ++kk) {
+            const int k = 32 * kk + 4 * quad + (l16 >> 2), at = (l16 & 3) * 8;
+            bf16x8 fm[CM], fn[TERMS][CN];
+#pragma unroll
+            for (int m = 0; m < CM; ++m) {
+                const unsigned char *p = s_codes + k * 256 + (((wx * CM + m) ^ (k & 7)) << 5) + at;
+                fm[m] = column(p, p + 16 * 256);
+            }
+#pragma unroll
+            for (int term = 0; term < TERMS; ++term)
+#pragma unroll
+                for (int n = 0; n < CN; ++n) {
+                    const unsigned char *p = s_y + term * YPLANE + k * YROW + (((wy * CN + n) ^ yswizzle(k)) << 5) + at;
+                    fn[term][n] = column(p, p + 16 * YROW);
+                }
+#pragma unroll
+            for (int term = TERMS - 1; term >= 0; --term)
+#pragma unroll
+                for (int m = 0; m < CM; ++m)
+#pragma unroll
+                    for (int n = 0; n < CN; ++n)
+                        acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fm[m], fn[term][n], acc[m][n], 0, 0, 0);
+        }
+    }
+    // a lane holds four columns of one row
+#pragma unroll
+    for (int n = 0; n < CN; ++n) {
+        const int r = r0 + (wy * CN + n) * 16 + l16;
+        if (r >= a.R) continue;
+#pragma unroll
+        for (int m = 0; m < CM; ++m) {
+            const int d = d0 + (wx * CM + m) * 16 + quad * 4, left = a.D - d;
+            if (left <= 0) continue;
+            if (!seg.whole) {
+                float *out = a.planes + (j * a.R + r) * (int64_t)a.D + d;
+                for (int i = 0; i < 4; ++i) if (i < left) out[i] = acc[m][n][i];
+            } else {
+                Out *out = (Out *)a.G + seg.e * a.ldG + (int64_t)r * a.D + d;
+                for (int i = 0; i < 4; ++i)
+                    if (i < left) {
+                        if (sizeof(Out) == 2) out[i] = (Out)bf16_bits(acc[m][n][i]); else out[i] = (Out)acc[m][n][i];
+                    }
+            }
+        }
+    }
+}
+
+// The planes of the examples of more than one segment, added in the order of their tokens.
+template <class Out>
+__global__ void __launch_bounds__(256)
+checkpoint_join_kernel(GradArgs a) {
+    const int64_t e = blockIdx.y, size = (int64_t)a.R * a.D, p0 = phi(a, e);
+    int64_t p1 = phi(a, e + 1);
+    if (p1 > a.segments) p1 = a.segments;
+    if (p1 - p0 < 2) return;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
+        float s = a.planes[p0 * size + i];
+        for (int64_t p = p0 + 1; p < p1; ++p) s = __fadd_rn(s, a.planes[p * size + i]);
+        Out *out = (Out *)a.G + e * a.ldG + i;
+        if (sizeof(Out) == 2) *out = (Out)bf16_bits(s); else *out = (Out)s;
+    }
+}
+
+// Tokens of a segment: enough segments to give every compute unit a few workgroups, but none so short that its plane (written and read,
+// 8 R bytes per column) costs more than its codes.
+static int64_t grad_chunk(int64_t T, int64_t n, int32_t R, int32_t D) {
+    const int64_t rtile = R > 64 ? 128 : R > 32 ? 64 : R > 16 ? 32 : 16;
+    const int64_t tiles = ((R + rtile - 1) / rtile) * ((D + kGroup - 1) / kGroup);
+    int64_t chunk = T * tiles / 1024;
+    if (chunk < 8 * (int64_t)R) chunk = 8 * (int64_t)R;
+    if (chunk < 128) chunk = 128;
+    if (n * tiles >= 512 && chunk < 4 * (T / n)) chunk = 4 * (T / n);      // enough workgroups: only an example far longer than the others is cut
+    if (chunk >= T) chunk = T + 1;
+    return (chunk + 63) / 64 * 64;
+}
+static int64_t grad_segments(int64_t T, int64_t n, int64_t chunk) { return n + T / chunk; }
+
+template <int RT, class Y, int TERMS, class Out>
+static qless_status launch_grad(GradArgs a, hipStream_t st) {
+    a.rtiles = (a.R + RT - 1) / RT;
+    a.dtiles = (a.D + kGroup - 1) / kGroup;
+    const int64_t grid = a.segments * a.rtiles * a.dtiles;
+    if (grid > 0x7FFFFFFF) return QLESS_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((checkpoint_grad_kernel<RT, Y, TERMS, Out>), dim3((unsigned)grid), dim3(256), 0, st, a);
+    if (a.segments > a.n) {
+        int64_t bx = ((int64_t)a.R * a.D + 1023) / 1024;
+        if (bx > 1024) bx = 1024;
+        hipLaunchKernelGGL(checkpoint_join_kernel<Out>, dim3((unsigned)bx, (unsigned)a.n), dim3(256), 0, st, a);
+    }
+    return launch_status();
+}
+template <class Y, int TERMS, class Out>
+static qless_status launch_grad_rows(const GradArgs &a, hipStream_t st) {
+    if (a.R <= 16) return launch_grad<16, Y, TERMS, Out>(a, st);
+    if (a.R <= 32) return launch_grad<32, Y, TERMS, Out>(a, st);
+    if (a.R <= 64) return launch_grad<64, Y, TERMS, Out>(a, st);
+    return launch_grad<128, Y, TERMS, Out>(a, st);
+}
+
+static bool checkpoint_shape_ok(int64_t T, int32_t D, int64_t ldX, int64_t ldC, int64_t ldS) {
+    return T >= 0 && D >= 1 && (T <= 1 || (ldX >= D && ldC >= D && ldS >= (D + (int64_t)kGroup - 1) / kGroup));
+}
+static unsigned checkpoint_grid(int64_t T, int32_t groups) {
+    const int64_t blocks = (T * groups + 15) / 16;
+    return (unsigned)(blocks < 4096 ? blocks : 4096);
+}
+
+}  // namespace qless
+
+extern "C" qless_status qless_checkpoint8(const void *X, qless_dtype dt, int64_t T, int32_t D, int64_t ldX, int8_t *codes, int64_t ldC,
+                                          float *step, int64_t ldS, void *stream) {
+    using namespace qless;
+    if (!checkpoint_shape_ok(T, D, ldX, ldC, ldS)) return QLESS_ERR_INVALID_ARG;
+    if (dt != QLESS_F32 && dt != QLESS_BF16) return QLESS_ERR_UNSUPPORTED;
+    if (T == 0) return QLESS_OK;
+    if (!X || !codes || !step) return QLESS_ERR_INVALID_ARG;
+    const int32_t groups = (D + kGroup - 1) / kGroup;
+    const hipStream_t st = (hipStream_t)stream;
+    if (dt == QLESS_F32)
+        hipLaunchKernelGGL(checkpoint_write_kernel<float>, dim3(checkpoint_grid(T, groups)), dim3(256), 0, st, (const float *)X, T, D, ldX, groups, codes, ldC, step, ldS);
+    else
+        hipLaunchKernelGGL(checkpoint_write_kernel<uint16_t>, dim3(checkpoint_grid(T, groups)), dim3(256), 0, st, (const uint16_t *)X, T, D, ldX, groups, codes, ldC, step, ldS);
+    return launch_status();
+}
+
+extern "C" qless_status qless_checkpoint8_read(const int8_t *codes, int64_t ldC, const float *step, int64_t ldS, int64_t T, int32_t D,
+                                               void *X, qless_dtype dt, int64_t ldX, void *stream) {
+    using namespace qless;
+    if (!checkpoint_shape_ok(T, D, ldX, ldC, ldS)) return QLESS_ERR_INVALID_ARG;
+    if (dt != QLESS_F32 && dt != QLESS_BF16) return QLESS_ERR_UNSUPPORTED;
+    if (T == 0) return QLESS_OK;
+    if (!X || !codes || !step) return QLESS_ERR_INVALID_ARG;
+    const int32_t groups = (D + kGroup - 1) / kGroup;
+    const hipStream_t st = (hipStream_t)stream;
+    if (dt == QLESS_F32)
+        hipLaunchKernelGGL(checkpoint_read_kernel<float>, dim3(checkpoint_grid(T, groups)), dim3(256), 0, st, codes, ldC, step, ldS, T, D, groups, (float *)X, ldX);
+    else
+        hipLaunchKernelGGL(checkpoint_read_kernel<uint16_t>, dim3(checkpoint_grid(T, groups)), dim3(256), 0, st, codes, ldC, step, ldS, T, D, groups, (uint16_t *)X, ldX);
+    return launch_status();
+}
+
+extern "C" size_t qless_checkpoint8_grad_workspace(int64_t T, int64_t n, int32_t R, int32_t D) {
+    using namespace qless;
+    if (T < 0 || n < 1 || R < 1 || D < 1) return 0;
+    const int64_t segments = grad_segments(T, n, grad_chunk(T, n, R, D));
+    return segments > n ? (size_t)segments * (size_t)R * (size_t)D * 4 : 0;
+}
+
+extern "C" qless_status qless_checkpoint8_grad(const void *dY, qless_dtype dtY, int64_t ldY, int32_t R, const int8_t *codes, int64_t ldC,
+                                               const float *step, int64_t ldS, int32_t D, int64_t T, const int64_t *offsets, int64_t n,
+                                               void *G, qless_dtype dtG, int64_t ldG, void *ws, size_t ws_bytes, void *stream) {
+    using namespace qless;
+    if (R < 1 || n < 0 || !checkpoint_shape_ok(T, D, D, ldC, ldS) || (T > 1 && ldY < R)) return QLESS_ERR_INVALID_ARG;
+    if ((dtY != QLESS_F32 && dtY != QLESS_BF16) || (dtG != QLESS_F32 && dtG != QLESS_BF16)) return QLESS_ERR_UNSUPPORTED;
+    if (n > 65535) return QLESS_ERR_UNSUPPORTED;
+    if (n > 1 && ldG < (int64_t)R * D) return QLESS_ERR_INVALID_ARG;
+    if (n == 0) return QLESS_OK;
+    if (!offsets || !G || (T > 0 && (!dY || !codes || !step))) return QLESS_ERR_INVALID_ARG;
+    GradArgs a{dY, ldY, codes, ldC, step, ldS, offsets, n, T, grad_chunk(T, n, R, D), 0, R, D, 0, 0, G, ldG, (float *)ws};
+    a.segments = grad_segments(T, n, a.chunk);
+    const size_t need = qless_checkpoint8_grad_workspace(T, n, R, D);
+    if (need > 0 && (!ws || ws_bytes < need || ((uintptr_t)ws & 15) != 0)) return QLESS_ERR_WORKSPACE;
+    const hipStream_t st = (hipStream_t)stream;
+    if (dtY == QLESS_BF16)
+        return dtG == QLESS_BF16 ? launch_grad_rows<uint16_t, 1, uint16_t>(a, st) : launch_grad_rows<uint16_t, 2, float>(a, st);
+    return dtG == QLESS_BF16 ? launch_grad_rows<float, 1, uint16_t>(a, st) : launch_grad_rows<float, 3, float>(a, st);
+}
