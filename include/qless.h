@@ -10,6 +10,7 @@
  *   qless_topk      Sec. 4.1      selection of the highest-scoring training examples
  *   qless_aggregate Sec. 4.1      maximum / mean of the influences over groups of validation examples
  * and, before them, what per-example gradients are made of:
+ *   qless_token_loss              loss over the vocabulary from the last hidden states, with its gradients
  *   qless_checkpoint8             activations kept in 8 bits from the forward to the backward pass
  *   qless_checkpoint8_grad        per-example weight gradients from them, as rows to project
  *
@@ -317,6 +318,32 @@ qless_status qless_score_groups(const void *const *train_codes, const float *con
                                 const float *eta, int C, int64_t N, int32_t M, int32_t k, int bits,
                                 const int32_t *group_end, int T, qless_agg mode, float *out,
                                 void *ws, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Loss of a batch of tokens over the vocabulary, with its gradients, from the last hidden states H (a row per token) and the
+ * head's weights W (a row per vocabulary entry); the T x V logits are never stored (a piece of the vocabulary at a time passes through
+ * the workspace).  With z_t = W H_t:
+ *   lse[t] = log sum_v exp z_tv        nll[t] = lse[t] - z_t,target[t]
+ *   L = sum_t weight[t] nll[t]:        dH = dL / dH,  dW = dL / dW
+ * A token whose target lies outside [0, V) (-100, say) is left out: nll, lse and its row of dH are 0, it adds nothing to dW, and its row
+ * of H and its weight are not read as numbers.
+ *   H, dH      device, T x D bfloat16, leading dimensions ldH, ldDH >= D
+ *   W, dW      device, V x D bfloat16, leading dimensions ldW, ldDW >= D
+ *   dt         QLESS_BF16 (others: QLESS_ERR_UNSUPPORTED);  1 <= D <= 65536,  T < 2^30
+ *   target     device, T int64           weight   device, T fp32 (the inverse of an example's count of targets, say), or NULL: 1
+ *   nll        device, T fp32            lse      device, T fp32, or NULL
+ *   dH, dW     either or both may be NULL; both are written whole, not added to
+ *   ws         device workspace, 16-byte aligned, of at least qless_token_loss_workspace(T, D, V, gradient) bytes; gradient:
+ *              non-zero if dH or dW is asked for
+ * Arithmetic: products of bfloat16 are exact, logits, maxima, sums and losses fp32; delta = weight (softmax - onehot) is rounded to
+ * bfloat16 once before the gradients' products, whose fp32 sums are rounded once.  Results are run-to-run identical.  Rows of W and H
+ * need no alignment beyond their elements'; W is read in place where its rows and D are whole 16-byte chunks, else copied piece by piece.
+ * A row of W outside the largest finite values makes every token's loss NaN or infinite, as the formulas do.
+ * ------------------------------------------------------------------------------------------- */
+size_t qless_token_loss_workspace(int64_t T, int32_t D, int32_t V, int gradient);
+qless_status qless_token_loss(const void *H, int64_t ldH, const void *W, int64_t ldW, qless_dtype dt, int64_t T, int32_t D, int32_t V,
+                              const int64_t *target, const float *weight, float *nll, float *lse, void *dH, int64_t ldDH,
+                              void *dW, int64_t ldDW, void *ws, size_t ws_bytes, void *stream);
 
 /* ---------------------------------------------------------------------------------------------
  * Activation checkpoints in 8 bits: a layer's input X (a row per token) is kept as codes and steps from the forward to

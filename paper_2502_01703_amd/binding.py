@@ -51,6 +51,9 @@ EXPORTS = {
     "qless_score_groups_workspace": (_sz, [_i64, _i32, _i32, _c.c_int, _c.c_int]),
     "qless_score_groups": (_c.c_int, [_vp, _vp, _vp, _vp, _vp, _c.c_int, _i64, _i32, _i32, _c.c_int, _vp, _c.c_int,
                                       _c.c_int, _vp, _vp, _sz, _vp]),
+    "qless_token_loss_workspace": (_sz, [_i64, _i32, _i32, _c.c_int]),
+    "qless_token_loss": (_c.c_int, [_vp, _i64, _vp, _i64, _c.c_int, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _i64,
+                                    _vp, _sz, _vp]),
     "qless_checkpoint8": (_c.c_int, [_vp, _c.c_int, _i64, _i32, _i64, _vp, _i64, _vp, _i64, _vp]),
     "qless_checkpoint8_read": (_c.c_int, [_vp, _i64, _vp, _i64, _i64, _i32, _vp, _c.c_int, _i64, _vp]),
     "qless_checkpoint8_grad_workspace": (_sz, [_i64, _i64, _i32, _i32]),
@@ -411,6 +414,36 @@ class _On:
     def __exit__(self, *_):
         if self.device.index != self.before:
             torch.cuda.set_device(self.before)
+
+
+def token_loss_workspace(T, D, V, gradient=True):
+    return int(lib().qless_token_loss_workspace(T, D, V, int(gradient)))
+
+
+def token_loss(H, W, target, weight=None, want_dH=True, want_dW=False, dH=None, dW=None, ws=None):
+    """qless_token_loss: last hidden states H [T, D] and head W [V, D] (bf16, row strides free), targets int64 [T] (outside
+    [0, V): left out), weights fp32 [T] or None -> (nll [T], lse [T], dH [T, D] or None, dW [V, D] or None)."""
+    ldH, ldW = _rows(H), _rows(W)
+    (T, D), V = H.shape, W.shape[0]
+    assert W.shape[1] == D and W.dtype == H.dtype
+    assert target.is_cuda and target.dtype == torch.int64 and target.shape == (T,) and target.is_contiguous()
+    assert weight is None or (weight.dtype == torch.float32 and weight.shape == (T,) and weight.is_contiguous())
+    with _On(H, W, target, weight, dH, dW, ws):
+        nll = torch.empty(T, dtype=torch.float32, device=H.device)
+        lse = torch.empty(T, dtype=torch.float32, device=H.device)
+        if want_dH and dH is None:
+            dH = torch.empty(T, D, dtype=H.dtype, device=H.device)
+        if want_dW and dW is None:
+            dW = torch.empty(V, D, dtype=W.dtype, device=H.device)
+        assert dH is None or (dH.shape == H.shape and dH.dtype == H.dtype)
+        assert dW is None or (dW.shape == W.shape and dW.dtype == W.dtype)
+        w = _ws(token_loss_workspace(T, D, V, dH is not None or dW is not None), H.device) if ws is None else ws
+        _check(lib().qless_token_loss(H.data_ptr(), ldH, W.data_ptr(), ldW, _dtype_code(H), T, D, V, target.data_ptr(),
+                                      weight.data_ptr() if weight is not None else None, nll.data_ptr(), lse.data_ptr(),
+                                      dH.data_ptr() if dH is not None else None, _rows(dH) if dH is not None else 0,
+                                      dW.data_ptr() if dW is not None else None, _rows(dW) if dW is not None else 0,
+                                      w.data_ptr(), w.numel(), _stream()), "qless_token_loss")
+    return nll, lse, dH, dW
 
 
 def checkpoint8(X, codes=None, step=None):

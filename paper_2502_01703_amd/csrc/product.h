@@ -1,0 +1,192 @@
+// Tiles of matrix products C[m][n] = sum_k A(m, k) B(n, k) of bfloat16 operands with fp32 sums, for the kernels whose epilogues are
+// more than a store.  An operand lies in memory by rows of K (ALONG: K contiguous, one row per m or n) or by rows of m or n (ACROSS: one
+// row per k); ACROSS operands are transposed by the LDS reads, so that neither form is ever rewritten in memory.
+//
+// A stage is 64 steps of K.  ALONG tiles lie in LDS as rows of 128 bytes, their eight 16-byte chunks exchanged by the row's bits 1 - 3
+// (16 rows read together use all banks); ACROSS tiles as 64 rows of the tile's width, their 64-byte pieces exchanged by the row's
+// bits 0 - 1 (the four rows that 32 lanes read together use all banks).  The stages are copied to LDS without passing through registers.
+#pragma once
+#include "common.h"
+
+namespace qless {
+
+typedef __attribute__((ext_vector_type(4))) short i16x4;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+
+enum { ALONG = 0, ACROSS = 1 };
+
+struct ProductOperand {
+    const void *base;          // 16-byte aligned
+    int64_t ld;                // bytes from row to row, a multiple of 16, below 2^23
+    int64_t extent;            // ALONG: rows that exist; ACROSS: bytes of a row that exist, a multiple of 16
+    int64_t depth;             // ALONG: bytes of a row that exist, a multiple of 16; ACROSS: rows that exist (below 2^31)
+};
+// What is read outside is replaced by what lies next to it inside: m and n past the extents give numbers that the epilogue leaves out;
+// where K ends inside a stage, one of the two operands has to hold zeros up to the stage's end.
+struct ProductArgs {
+    ProductOperand a, b;
+    int64_t n;                 // columns of C
+    int64_t k;                 // steps of K
+    const int32_t *live_n, *live_k;   // device: fewer of them, or null (k rounded up to a stage: the operands are zero there)
+    int32_t mtiles, splits;    // splits: K in as many parts of whole stages
+};
+
+template <int KIND, int EXT, int NW> struct ProductCopies {
+    static constexpr int BYTES = EXT * 128, Q = EXT / 8, U = (Q + NW - 1) / NW;     // copies of 1 KB, per wavefront
+    const unsigned char *base;
+    int ld, short_stage, left_there;                       // the stage that K ends in, if it is not whole, and what it holds
+    unsigned off[U];
+    __device__ inline void init(const ProductOperand &op, int first, int lane, int wave) {
+        constexpr int WHOLE = KIND == ALONG ? 128 : 64;
+        ld = (int)op.ld;
+        left_there = (int)op.depth % WHOLE;
+        short_stage = left_there ? (int)op.depth / WHOLE : -1;
+        base = (const unsigned char *)op.base + (KIND == ALONG ? (int64_t)first * ld : (int64_t)first * 2);
+        const int64_t there = KIND == ALONG ? op.extent - 1 - first : op.extent - (int64_t)first * 2 - 16;     // of rows, or of a row's bytes
+        const int left = there < 65536 ? (int)there : 65536;   // more than a tile
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            int row, chunk;
+            place(u, lane, wave, row, chunk);
+            off[u] = KIND == ALONG ? (unsigned)((row < left ? row : left) * ld) + chunk : (unsigned)(row * ld) + (unsigned)(chunk < left ? chunk : left);
+        }
+    }
+    static __device__ inline void place(int u, int lane, int wave, int &row, int &chunk) {
+        int q = wave * U + u;
+        if (Q % (NW * U) != 0 && q > Q - 1) q = Q - 1;     // repeats the last copy: all wavefronts count alike
+        if (KIND == ALONG) {
+            row = 8 * q + (lane >> 3);
+            chunk = ((lane & 7) ^ ((row >> 1) & 7)) * 16;
+        } else {
+            constexpr int LANES = EXT / 8;                 // of a row
+            row = q * (64 / LANES) + lane / LANES;
+            chunk = ((lane % LANES) ^ ((row & 3) << 2)) * 16;
+        }
+    }
+    // copy u of stage s to its place in the stage at `lds`
+    __device__ inline void issue(int u, int s, int lane, int wave, unsigned lds) const {
+        int q = wave * U + u;
+        if (Q % (NW * U) != 0 && q > Q - 1) q = Q - 1;
+        const unsigned char *from = base + (KIND == ALONG ? (int64_t)s * 128 : (int64_t)s * 64 * ld);
+        unsigned at = off[u];
+        if (s == short_stage) {                            // the same for all lanes
+            const int left = left_there;
+            int row, chunk;
+            place(u, lane, wave, row, chunk);
+            if (KIND == ALONG) at -= (unsigned)(chunk < left ? 0 : chunk - (left - 16));
+            else at -= (unsigned)((row < left ? 0 : row - (left - 1)) * ld);
+        }
+        global_to_lds16(from, at, lds + (unsigned)(q * 1024));
+    }
+};
+
+// A fragment: for 32 rows of the tile from `first` on (a multiple of 32), eight steps of K per lane.
+template <int KIND, int EXT>
+__device__ inline unsigned fragment_lane(int lane) {
+    const int half = lane >> 5, l32 = lane & 31, l16 = lane & 15;
+    if (KIND == ALONG) return (unsigned)(l32 * 128 + ((half ^ ((l32 >> 1) & 7)) << 4));
+    const int row = 8 * half + (l16 >> 2);
+    return (unsigned)(row * EXT * 2 + (l16 >> 2) * 64 + ((lane >> 4) & 1) * 32 + (l16 & 3) * 8);
+}
+template <int KIND, int EXT>
+__device__ inline bf16x8 fragment(const unsigned char *stage, unsigned lane_at, int first, int kk) {
+    if (KIND == ALONG) return *(const bf16x8 *)(stage + first * 128 + (lane_at ^ (unsigned)(kk << 5)));
+    typedef __attribute__((address_space(3))) i16x4 lds16x4;
+    const unsigned char *p = stage + kk * (16 * EXT * 2) + (lane_at ^ (unsigned)(first * 2));
+    const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)p);
+    const i16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)(p + 4 * EXT * 2));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// MT x NT tiles by WY x WX wavefronts with FM x FN accumulators of 32 x 32 each, NS stages in LDS.
+template <int MT_, int NT_, int WY_, int WX_, int NS_> struct ProductShape {
+    static constexpr int MT = MT_, NT = NT_, WY = WY_, WX = WX_, NS = NS_, NW = WY * WX, FM = MT / WY / 32, FN = NT / WX / 32;
+    static constexpr int STAGE = (MT + NT) * 128, LDS = NS * STAGE;
+    static_assert(FM * WY * 32 == MT && FN * WX * 32 == NT && NS >= 2, "whole fragments");
+};
+
+// Epilogue::run(args, acc, m, n, split, live): acc[i][j][v] is C at m + 32 i + 8 (v / 4) + 4 half + v % 4, n + 32 j + lane % 32.
+template <class Sh, int AK, int BK, class Epilogue>
+__global__ void __launch_bounds__(64 * Sh::NW, Sh::NW / 4)
+product_kernel(ProductArgs p, typename Epilogue::Args e) {
+    constexpr int FM = Sh::FM, FN = Sh::FN, NS = Sh::NS, NW = Sh::NW;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    // Tiles in an order in which the workgroups of an XCD (ids eight apart) share operands: bands of eight column tiles, row tile by row
+    // tile, an eighth of the order each.
+    const int64_t n = p.live_n ? *p.live_n : p.n;
+    const int64_t k = p.live_k ? *p.live_k : p.k;
+    const int64_t ntiles = (n + Sh::NT - 1) / Sh::NT, plane = p.mtiles * ntiles, total = plane * p.splits, per = (total + 7) / 8;
+    const int64_t id = blockIdx.x, idx = (id & 7) * per + (id >> 3);
+    if ((id >> 3) >= per || idx >= total) return;          // the whole workgroup
+    const int split = __builtin_amdgcn_readfirstlane((int)(idx / plane));
+    const int64_t in = idx - split * plane, band = in / (8 * p.mtiles), wide = ntiles - band * 8 < 8 ? ntiles - band * 8 : 8, r = in - band * 8 * p.mtiles;
+    const int m0 = __builtin_amdgcn_readfirstlane((int)(r / wide * Sh::MT)), n0 = __builtin_amdgcn_readfirstlane((int)((band * 8 + r % wide) * Sh::NT));
+    const int64_t stages = (k + 63) / 64;
+    const int s0 = __builtin_amdgcn_readfirstlane((int)(stages * split / p.splits)), s1 = __builtin_amdgcn_readfirstlane((int)(stages * (split + 1) / p.splits));
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wy = wave / Sh::WX, wx = wave % Sh::WX;
+    const unsigned lds0 = (unsigned)(uintptr_t)((__attribute__((address_space(3))) unsigned char *)smem);
+    ProductCopies<AK, Sh::MT, NW> ca;
+    ProductCopies<BK, Sh::NT, NW> cb;
+    constexpr int UA = ProductCopies<AK, Sh::MT, NW>::U, UB = ProductCopies<BK, Sh::NT, NW>::U;
+    ca.init(p.a, m0, lane, wave);
+    cb.init(p.b, n0, lane, wave);
+    auto request = [&](int s, int slot) {
+        if (s > s1 - 1) s = s1 - 1;                        // repeated past the end: all stages count alike
+        const unsigned at = lds0 + (unsigned)(slot * Sh::STAGE);
+#pragma unroll
+        for (int u = 0; u < UA; ++u) ca.issue(u, s, lane, wave, at);
+#pragma unroll
+        for (int u = 0; u < UB; ++u) cb.issue(u, s, lane, wave, at + Sh::MT * 128);
+    };
+    f32x16 acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+    const unsigned la = fragment_lane<AK, Sh::MT>(lane), lb = fragment_lane<BK, Sh::NT>(lane);
+    const int ma = wy * FM * 32, nb = wx * FN * 32;
+    if (s0 < s1) {
+#pragma unroll
+        for (int i = 0; i < NS - 1; ++i) request(s0 + i, i);
+        int slot = 0;
+        for (int s = s0; s < s1; ++s) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            wait_vmcnt<(NS - 2) * (UA + UB)>();            // this wavefront's share of the stage has landed
+            __builtin_amdgcn_s_barrier();                  // everyone's; and everyone has read the slot that is requested next
+            asm volatile("" ::: "memory");
+            request(s + NS - 1, slot == 0 ? NS - 1 : slot - 1);
+            const unsigned char *sa = smem + slot * Sh::STAGE, *sb = sa + Sh::MT * 128;
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+                bf16x8 fa[FM], fb[FN];
+#pragma unroll
+                for (int i = 0; i < FM; ++i) fa[i] = fragment<AK, Sh::MT>(sa, la, ma + 32 * i, kk);
+#pragma unroll
+                for (int j = 0; j < FN; ++j) fb[j] = fragment<BK, Sh::NT>(sb, lb, nb + 32 * j, kk);
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+            }
+            slot = slot + 1 == NS ? 0 : slot + 1;
+        }
+        wait_vmcnt<0>();                                   // no copy is under way when the workgroup gives its LDS back
+    }
+    Epilogue::template run<FM, FN>(e, acc, m0 + ma, n0 + nb, split, n);
+}
+
+template <class Sh, int AK, int BK, class Epilogue>
+static qless_status launch_product(const ProductArgs &p, const typename Epilogue::Args &e, hipStream_t st) {
+    QLESS_LDS_KERNEL((product_kernel<Sh, AK, BK, Epilogue>), Sh::LDS);
+    const int64_t total = p.mtiles * ((p.n + Sh::NT - 1) / Sh::NT) * p.splits, grid = (total + 7) / 8 * 8;
+    if (grid > 0x7FFFFFFF) return QLESS_ERR_UNSUPPORTED;
+    if (grid > 0)
+        hipLaunchKernelGGL((product_kernel<Sh, AK, BK, Epilogue>), dim3((unsigned)grid), dim3(64 * Sh::NW), Sh::LDS, st, p, e);
+    return QLESS_OK;
+}
+
+}  // namespace qless

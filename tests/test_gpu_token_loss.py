@@ -1,0 +1,210 @@
+"""The loss over the vocabulary and its gradients against their formulas in 64 bits.
+
+Bounds.  A logit is a sum of D exact products added in fp32, each of at most D + 64 additions off by at most one step of a partial sum:
+|error| <= ez = (D + 64) 2^-23 max_v sum_d |h w|.  A sum of exponentials is relative 2^-15 off at most (fewer than 200 additions on any
+path, each 2^-23, and exponentials of arguments that were rounded), its logarithm as much absolutely: lse within ez + 2^-15 + 2^-22 |lse|,
+nll within twice that (el).  A probability is then relative er = 3 (el + 2^-15) off, delta = weight (softmax - onehot) by that and by its
+rounding to bfloat16, 2^-8 of itself; a gradient sums these errors, adds its own fp32 sums' (count of terms + 64) 2^-23 of the terms and
+the rounding of the result, 2^-8 of it."""
+import pytest
+import torch
+
+from paper_2502_01703_amd import binding as Q
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def _say(msg):
+    print("[case] " + msg, flush=True)
+
+
+def _inside(X, left, right):
+    wide = torch.full((X.shape[0], left + X.shape[1] + right), 7, dtype=X.dtype, device=DEV)
+    wide[:, left:left + X.shape[1]] = X.to(DEV)
+    return wide[:, left:left + X.shape[1]], wide
+
+
+def _inputs(T, D, V, seed, masked=0.3, scale=4.0):
+    g = torch.Generator().manual_seed(seed)
+    W = torch.randn(V, D, generator=g) / D ** 0.5
+    y = torch.randint(0, V, (T,), generator=g)
+    H = torch.randn(T, D, generator=g) + 2 * scale * torch.rand(T, 1, generator=g) * W[y]
+    out = torch.rand(T, generator=g) < masked
+    y[out] = torch.tensor([-100, -1, V, 1 << 40])[torch.randint(0, 4, (int(out.sum()),), generator=g)]
+    w = torch.rand(T, generator=g) - 0.2
+    return H.bfloat16().to(DEV), W.bfloat16().to(DEV), y.to(DEV), w.to(DEV)
+
+
+def _check(H, W, y, w, got):
+    """All outputs of a call within the bounds above."""
+    nll, lse, dH, dW = got
+    live = ((y >= 0) & (y < W.shape[0])).nonzero()[:, 0]
+    rest = torch.ones(len(y), dtype=torch.bool, device=DEV)
+    rest[live] = False
+    assert not nll[rest].any() and not lse[rest].any()
+    assert dH is None or not dH[rest].any()
+    if len(live) == 0:
+        assert dW is None or not dW.any()
+        return
+    h, W64, t = H[live].double(), W.double(), y[live][:, None]
+    D, V = W.shape[1], W.shape[0]
+    z = torch.mm(h, W64.t().contiguous())
+    ez = (D + 64) * 2.0 ** -23 * torch.mm(h.abs(), W64.abs().t().contiguous()).amax(1)
+    ref_lse = torch.logsumexp(z, 1)
+    ref = ref_lse - z.gather(1, t)[:, 0]
+    el = 2 * (ez + 2.0 ** -15 + 2.0 ** -22 * ref_lse.abs())
+    assert ((lse[live].double() - ref_lse).abs() <= el).all()
+    assert ((nll[live].double() - ref).abs() <= el).all()
+    if dH is None and dW is None:
+        return
+    er = 3 * (el + 2.0 ** -15)[:, None]
+    weight = torch.ones(len(live), device=DEV, dtype=torch.float64) if w is None else w[live].double()
+    p = torch.softmax(z, 1)
+    hot = torch.zeros_like(p).scatter_(1, t, 1.0)
+    delta = p.scatter(1, t, torch.special.expm1(-ref)[:, None]) * weight[:, None]
+    off = 2.0 ** -8 * delta.abs() + weight.abs()[:, None] * (p + hot) * er * (1 + 2.0 ** -8)
+    if dH is not None:
+        r = torch.mm(delta, W64)
+        bound = torch.mm(off, W64.abs()) + (V + 64) * 2.0 ** -23 * torch.mm(delta.abs() + off, W64.abs())
+        assert ((dH[live].double() - r).abs() <= bound + 2.0 ** -8 * (r.abs() + bound)).all()
+    if dW is not None:
+        r = torch.mm(delta.t().contiguous(), h)
+        bound = torch.mm(off.t().contiguous(), h.abs()) + (len(live) + 64) * 2.0 ** -23 * torch.mm((delta.abs() + off).t().contiguous(), h.abs())
+        assert ((dW.double() - r).abs() <= bound + 2.0 ** -8 * (r.abs() + bound)).all()
+
+
+SIZES = [(1, 1, 1), (1, 64, 2), (1, 8, 1000), (2, 72, 257), (1, 4096, 300), (31, 100, 256), (32, 128, 2049), (33, 520, 255), (257, 129, 1000), (300, 64, 513),
+         (300, 264, 3001), (513, 8, 700), (64, 1000, 5000)]
+
+
+@pytest.mark.parametrize("T,D,V", SIZES)
+@pytest.mark.parametrize("pads", [(0, 0), (8, 16), (3, 1)])
+def test_loss_and_gradients(T, D, V, pads):
+    _say("loss T=%d D=%d V=%d pads=%s" % (T, D, V, pads))
+    H, W, y, w = _inputs(T, D, V, T + D + V, masked=0.0 if T == 1 else 0.3)
+    h, _ = _inside(H, pads[0], 1 if pads[0] else 0)
+    W_, _ = _inside(W, pads[1], 0)
+    dH, wideH = _inside(torch.zeros_like(H), pads[1], 2)
+    dW, wideW = _inside(torch.zeros_like(W), pads[0], 2)
+    ws = torch.full((Q.token_loss_workspace(T, D, V),), 0xFF, dtype=torch.uint8, device=DEV)     # NaN wherever it is read unwritten
+    got = Q.token_loss(h, W_, y, w, dH=dH, dW=dW, ws=ws)
+    _check(H, W, y, w, got)
+    for wide, left, n in ((wideH, pads[1], D), (wideW, pads[0], D)):         # what lies beside the rows stays
+        assert (wide[:, :left] == 7).all() and (wide[:, left + n:] == 7).all()
+    # each output alone, and without weights
+    for want in ((False, False), (True, False), (False, True)):
+        alone = Q.token_loss(h, W_, y, w, want_dH=want[0], want_dW=want[1])
+        assert torch.equal(alone[0], got[0]) and torch.equal(alone[1], got[1])
+        _check(H, W, y, w, alone)
+    _check(H, W, y, None, Q.token_loss(h, W_, y))
+
+
+@pytest.mark.parametrize("T,D,V", [(8192, 64, 20000), (1, 4100, 20000), (2000, 72, 70000), (700, 100, 150000)])
+def test_pieces_of_the_vocabulary(T, D, V):
+    """More vocabulary than a piece holds, read in place and packed."""
+    _say("loss pieces T=%d D=%d V=%d" % (T, D, V))
+    H, W, y, w = _inputs(T, D, V, V, masked=0.2 if T > 1 else 0.0)
+    _check(H, W, y, w, Q.token_loss(H, W, y, w, want_dW=True))
+
+
+@pytest.mark.parametrize("T", [3, 100])
+def test_no_target_at_all(T):
+    _say("loss without targets T=%d" % T)
+    H, W, y, w = _inputs(T, 72, 300, 4)
+    got = Q.token_loss(torch.full_like(H, float("nan")), W, torch.full_like(y, -100), torch.full_like(w, float("nan")), want_dW=True)
+    for x in got:
+        assert not x.any()
+    empty = Q.token_loss(H[:0], W, y[:0], w[:0], want_dW=True)
+    assert empty[0].shape == (0,) and empty[2].shape == (0, 72) and not empty[3].any()
+
+
+def test_left_out_rows_are_not_read_as_numbers():
+    _say("loss with NaN in rows that are left out")
+    H, W, y, w = _inputs(290, 136, 777, 5, masked=0.6)
+    want = Q.token_loss(H, W, y, w, want_dW=True)
+    out = (y < 0) | (y >= 777)
+    H[out], w[out] = float("nan"), float("inf")
+    for a, b in zip(want, Q.token_loss(H, W, y, w, want_dW=True)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("scale", [0.0, 60.0, 3000.0])
+def test_certain_and_hopeless_tokens(scale):
+    """Losses of nearly nothing keep their digits, losses of thousands do not overflow."""
+    _say("loss scale %g" % scale)
+    H, W, y, w = _inputs(130, 256, 1000, 6, masked=0.1, scale=scale)
+    H[::3] = -H[::3]
+    _check(H, W, y, w, Q.token_loss(H, W, y, w, want_dW=True))
+
+
+def test_one_bad_token():
+    """A token whose hidden state is not finite spoils its own loss and row only (and dW)."""
+    _say("loss with one token not finite")
+    H, W, y, w = _inputs(70, 64, 500, 7, masked=0.0)
+    want = Q.token_loss(H, W, y, w)
+    H[13, 5] = float("nan")
+    got = Q.token_loss(H, W, y, w)
+    good = torch.arange(70, device=DEV) != 13
+    for a, b in zip(want[:3], got[:3]):
+        assert torch.equal(a[good], b[good]) and b[13].isnan().all()
+
+
+def test_gradient_against_differences():
+    """dH and dW against differences of the summed loss along a direction."""
+    _say("loss differences")
+    H, W, y, w = _inputs(40, 96, 400, 8)
+    _, _, dH, dW = Q.token_loss(H, W, y, w, want_dW=True)
+
+    def L(h, W_):
+        nll, _, _, _ = Q.token_loss(h, W_, y, w, want_dH=False)
+        live = (y >= 0) & (y < 400)
+        return (nll.double() * torch.where(live, w, torch.zeros_like(w)).double()).sum()
+    # a step of bfloat16 numbers: H and W moved to neighbours along their gradients' signs
+    for X, G, f in ((H, dH, lambda x: L(x, W)), (W, dW, lambda x: L(H, x))):
+        up, down = (X.float() + 0.02 * X.float().abs() * G.float().sign()).bfloat16(), (X.float() - 0.02 * X.float().abs() * G.float().sign()).bfloat16()
+        first = ((up.double() - down.double()) * G.double()).sum()
+        d = (f(up) - f(down)).double()
+        # the third derivative of a softmax along a step of logits of size s is at most s^3; logits move by at most s here
+        s = 0.03 * torch.mm(H.float().abs(), W.float().abs().t().contiguous()).amax(1).double()
+        slack = (w.abs().double() * s ** 3).sum() + 2.0 ** -7 * ((up.double() - down.double()) * G.double()).abs().sum() + 1e-3
+        assert (d - first).abs() <= slack
+
+
+def test_replayed_in_a_graph():
+    _say("loss in a graph")
+    Q.init()
+    H, W, y, w = _inputs(70, 200, 1500, 9)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        Q.token_loss(H, W, y, w, want_dW=True)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = Q.token_loss(H, W, y, w, want_dW=True)
+    for i in range(4):
+        _say("loss replay %d" % i)
+        a, b, c, d = _inputs(70, 200, 1500, 10 + i, masked=0.25 * i)
+        H.copy_(a), W.copy_(b), y.copy_(c), w.copy_(d)
+        graph.replay()
+        torch.cuda.synchronize()
+        kept = [x.clone() for x in held]
+        for p, q in zip(kept, Q.token_loss(H, W, y, w, want_dW=True)):
+            assert torch.equal(p, q)
+
+
+def test_other_stream_and_shared_workspace():
+    """Calls in a row on one workspace, on a stream of their own."""
+    _say("loss on another stream")
+    ws = torch.full((Q.token_loss_workspace(300, 264, 3001),), 0xFF, dtype=torch.uint8, device=DEV)
+    s = torch.cuda.Stream()
+    for T, D, V in ((300, 264, 3001), (5, 64, 100), (33, 72, 1000)):
+        H, W, y, w = _inputs(T, D, V, T)
+        want = Q.token_loss(H, W, y, w, want_dW=True)
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            got = Q.token_loss(H, W, y, w, want_dW=True, ws=ws)
+        s.synchronize()
+        for a, b in zip(want, got):
+            assert torch.equal(a, b)

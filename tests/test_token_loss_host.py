@@ -1,0 +1,33 @@
+"""The loss over the vocabulary, without a GPU: what the entry point refuses."""
+import ctypes
+
+from paper_2502_01703_amd import binding
+
+OK, INVALID, UNSUPPORTED, WORKSPACE = 0, 1, 2, 3
+one = ctypes.c_void_p(16)           # never dereferenced: every call below ends on the host
+
+
+def test_refusals():
+    L = binding.lib()
+
+    def call(H=one, ldH=64, W=one, ldW=64, dt=1, T=4, D=64, V=100, target=one, weight=None, nll=one, lse=None, dH=one, ldDH=64, dW=one, ldDW=64,
+             ws=one, wsb=1 << 40):
+        return L.qless_token_loss(H, ldH, W, ldW, dt, T, D, V, target, weight, nll, lse, dH, ldDH, dW, ldDW, ws, wsb, None)
+    for bad in (dict(T=-1), dict(D=0), dict(V=0), dict(ldH=63), dict(ldW=63), dict(ldDH=63), dict(ldDW=63), dict(H=None), dict(W=None),
+                dict(target=None), dict(nll=None)):
+        assert call(**bad) == INVALID, bad
+    for bad in (dict(dt=0), dict(dt=2), dict(D=65537, ldH=65537, ldW=65537, ldDH=65537, ldDW=65537), dict(T=1 << 30)):
+        assert call(**bad) == UNSUPPORTED, bad
+    need = L.qless_token_loss_workspace(4, 64, 100, 1)
+    assert need > L.qless_token_loss_workspace(4, 64, 100, 0) > 0
+    for bad in (dict(wsb=need - 1), dict(ws=None), dict(ws=ctypes.c_void_p(24))):
+        assert call(**bad) == WORKSPACE, bad
+    assert call(T=0, dW=None, H=None, target=None, nll=None, ws=None, wsb=0) == OK
+    for shape in ((-1, 64, 100, 1), (4, 0, 100, 1), (4, 64, 0, 1)):
+        assert L.qless_token_loss_workspace(*shape) == 0
+
+
+def test_workspace_does_not_hold_the_logits():
+    L = binding.lib()
+    T, D, V = 65536, 4096, 131072
+    assert L.qless_token_loss_workspace(T, D, V, 1) < T * V * 2 // 4
