@@ -333,14 +333,15 @@ qless_status qless_score_groups(const void *const *train_codes, const float *con
  *   target     device, T int64           weight   device, T fp32 (the inverse of an example's count of targets, say), or NULL: 1
  *   nll        device, T fp32            lse      device, T fp32, or NULL
  *   dH, dW     either or both may be NULL; both are written whole, not added to
- *   ws         device workspace, 16-byte aligned, of at least qless_token_loss_workspace(T, D, V, gradient) bytes; gradient:
- *              non-zero if dH or dW is asked for
- * Arithmetic: products of bfloat16 are exact, logits, maxima, sums and losses fp32; delta = weight (softmax - onehot) is rounded to
- * bfloat16 once before the gradients' products, whose fp32 sums are rounded once.  Results are run-to-run identical.  Rows of W and H
+ *   ws         device workspace, 16-byte aligned, of at least qless_token_loss_workspace(T, D, V, want_dH, want_dW) bytes; want_dH,
+ *              want_dW: non-zero if dH (dW) is asked for
+ * Arithmetic: products of bfloat16 are exact, logits, maxima, sums and losses fp32.  In the gradients a target's entry of
+ * weight (softmax - onehot) is fp32, the others are rounded to bfloat16 once (up to 32 tokens: to two bfloat16 terms); sums are fp32 and
+ * rounded once.  Results are run-to-run identical.  Rows of W and H
  * need no alignment beyond their elements'; W is read in place where its rows and D are whole 16-byte chunks, else copied piece by piece.
  * A row of W outside the largest finite values makes every token's loss NaN or infinite, as the formulas do.
  * ------------------------------------------------------------------------------------------- */
-size_t qless_token_loss_workspace(int64_t T, int32_t D, int32_t V, int gradient);
+size_t qless_token_loss_workspace(int64_t T, int32_t D, int32_t V, int want_dH, int want_dW);
 qless_status qless_token_loss(const void *H, int64_t ldH, const void *W, int64_t ldW, qless_dtype dt, int64_t T, int32_t D, int32_t V,
                               const int64_t *target, const float *weight, float *nll, float *lse, void *dH, int64_t ldDH,
                               void *dW, int64_t ldDW, void *ws, size_t ws_bytes, void *stream);

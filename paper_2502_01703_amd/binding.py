@@ -51,7 +51,7 @@ EXPORTS = {
     "qless_score_groups_workspace": (_sz, [_i64, _i32, _i32, _c.c_int, _c.c_int]),
     "qless_score_groups": (_c.c_int, [_vp, _vp, _vp, _vp, _vp, _c.c_int, _i64, _i32, _i32, _c.c_int, _vp, _c.c_int,
                                       _c.c_int, _vp, _vp, _sz, _vp]),
-    "qless_token_loss_workspace": (_sz, [_i64, _i32, _i32, _c.c_int]),
+    "qless_token_loss_workspace": (_sz, [_i64, _i32, _i32, _c.c_int, _c.c_int]),
     "qless_token_loss": (_c.c_int, [_vp, _i64, _vp, _i64, _c.c_int, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _i64,
                                     _vp, _sz, _vp]),
     "qless_checkpoint8": (_c.c_int, [_vp, _c.c_int, _i64, _i32, _i64, _vp, _i64, _vp, _i64, _vp]),
@@ -416,8 +416,8 @@ class _On:
             torch.cuda.set_device(self.before)
 
 
-def token_loss_workspace(T, D, V, gradient=True):
-    return int(lib().qless_token_loss_workspace(T, D, V, int(gradient)))
+def token_loss_workspace(T, D, V, want_dH=True, want_dW=False):
+    return int(lib().qless_token_loss_workspace(T, D, V, int(want_dH), int(want_dW)))
 
 
 def token_loss(H, W, target, weight=None, want_dH=True, want_dW=False, dH=None, dW=None, ws=None):
@@ -437,7 +437,7 @@ def token_loss(H, W, target, weight=None, want_dH=True, want_dW=False, dH=None, 
             dW = torch.empty(V, D, dtype=W.dtype, device=H.device)
         assert dH is None or (dH.shape == H.shape and dH.dtype == H.dtype)
         assert dW is None or (dW.shape == W.shape and dW.dtype == W.dtype)
-        w = _ws(token_loss_workspace(T, D, V, dH is not None or dW is not None), H.device) if ws is None else ws
+        w = _ws(token_loss_workspace(T, D, V, dH is not None, dW is not None), H.device) if ws is None else ws
         _check(lib().qless_token_loss(H.data_ptr(), ldH, W.data_ptr(), ldW, _dtype_code(H), T, D, V, target.data_ptr(),
                                       weight.data_ptr() if weight is not None else None, nll.data_ptr(), lse.data_ptr(),
                                       dH.data_ptr() if dH is not None else None, _rows(dH) if dH is not None else 0,

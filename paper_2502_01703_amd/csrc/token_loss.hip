@@ -3,9 +3,17 @@
 //   z = H W^T,  lse_t = log sum_v exp z_tv,  nll_t = lse_t - z_t,target,  delta_tv = w_t (exp(z_tv - lse_t) - [v = target_t]),
 //   dH = delta W,  dW = delta^T H.
 // Tokens without a target in the vocabulary are left out: the others' rows of H are gathered first (bounded by T on the host, counted
-// on the device), so that a prompt costs no products.  A first pass over the vocabulary keeps each token's maximum and sum of 256
-// logits at a time; a second one, a piece of the vocabulary after another, forms the logits again and leaves delta of the piece as
-// bfloat16 in the workspace, which the products for dH and dW read.
+// on the device), so that a prompt costs no products.
+//
+// Loss alone: the tiles of logits end with the maximum and the sum of their exponentials, which are joined.
+// dH: a piece of the vocabulary at a time, the logits of the piece (fp32, in the workspace, small enough to stay in the last-level cache)
+// become p = exp(z - m) with the running maximum m, and planes = planes exp(m_before - m) + p W: one pass over the vocabulary, as with
+// the running softmax of an attention.  dH = w / s planes + w (p_target - 1) W_target at the end.
+// dW needs lse first.  Where the whole vocabulary is one piece, delta is final at once; else a second pass forms the logits again.
+//
+// The target's entry, the largest of a row, never passes through the bfloat16 operand: it is added in fp32, to dH in the last kernel,
+// to dW behind the product, from the tokens ordered by target.  (Rounded with the rest it made gradients of few tokens up to 0.4 %
+// wrong.)  Up to 32 tokens, where the products wait for W anyway, the rest goes in as the sum of two bfloat16 numbers.
 #include "product.h"
 #include "score.h"
 
@@ -16,18 +24,24 @@ struct LossTokens {                        // workspace views, by live token (pa
     int32_t *count;                        // live tokens
     int32_t *token, *target;               // [Tp]
     int32_t *place;                        // [T]: live index of a token, or -1
-    float *weight, *lse, *nll, *hit;       // [Tp]; hit: the target's logit
+    float *weight, *lse, *hit;             // [Tp]; hit: the target's logit
+    float *top, *sum, *shrink;             // [Tp] running maximum and sum; exp of the last change of the maximum
+    float *pull;                           // [Tp] w (p_target - 1)
     float2 *part;                          // [parts][Tp] maximum, sum of exp(z - maximum)
-    uint16_t *delta;                       // [Tp][Vc]
-    uint16_t *pack;                        // [Vc][Dp] where W cannot be read as it lies
+    int32_t *order, *order_target, *start; // [Tp] live tokens by target, and their targets; [Vp / 64 + 1]: where each 64 entries begin there
+    float *logits;                         // [Tp][piece]
+    uint16_t *delta;                       // [Tp][piece]
+    uint16_t *pack;                        // [piece][Dp] where W cannot be read as it lies
     float *planes;                         // [splits][Tp][Dp] partial dH
 };
 struct LossPlan {
-    int64_t T, Tp, Dp, Vp, Vc, parts;
+    int64_t T, Tp, Dp, Vp, piece, parts;
     int32_t D, V, tile_n, splits;
-    bool packed;
-    size_t off[12], total;
+    bool one_pass;                         // dW without a second pass
+    size_t off[18], total;
 };
+
+constexpr int kFew = 32;                   // tokens up to which the rest of delta is two terms: rows t and t + kFew of delta and H
 
 constexpr int kLossThreads = 1024;
 
@@ -81,13 +95,13 @@ loss_live_kernel(const int64_t *target, const float *weight, int64_t T, int32_t 
 }
 
 // Rows of bfloat16 copied to rows of ld (a multiple of 64) with zeros behind their D elements, eight elements a thread; `from` null: row r,
-// else the row that it names, and zeros from *count up to whole tiles.
+// else the row that it names, and zeros from *count up to whole tiles; few: rows from kFew on repeat the first ones.
 __global__ void __launch_bounds__(256)
-loss_rows_kernel(const uint16_t *X, int64_t ldX, int32_t D, const int32_t *from, const int32_t *count, int64_t rows, uint16_t *out, int64_t ld) {
-    const int64_t r = blockIdx.x;
+loss_rows_kernel(const uint16_t *X, int64_t ldX, int32_t D, const int32_t *from, const int32_t *count, int64_t rows, int few, uint16_t *out, int64_t ld) {
+    const int64_t r = blockIdx.x, of = few && r >= kFew ? r - kFew : r;
     const int64_t n = count ? *count : rows;
-    if (r >= (n + 255) / 256 * 256) return;
-    const uint16_t *x = r < n ? X + (from ? (int64_t)from[r] : r) * ldX : nullptr;
+    if (r >= (n + 255) / 256 * 256 && !few) return;
+    const uint16_t *x = of < n ? X + (from ? (int64_t)from[of] : of) * ldX : nullptr;
     for (int64_t c = threadIdx.x * 8; c < ld; c += 256 * 8) {
         uint16_t v[8];
 #pragma unroll
@@ -101,12 +115,13 @@ loss_rows_kernel(const uint16_t *X, int64_t ldX, int32_t D, const int32_t *from,
 }
 
 // ---- what the tiles of logits end with: rows m are vocabulary entries, columns n tokens
-struct LossStats {
-    struct Args { const int32_t *target; float *hit; float2 *part; int64_t Tp, first; int32_t V; };
+template <bool STORE> struct LossStats {
+    struct Args { const int32_t *target; float *hit; float2 *part; int64_t Tp, first; int32_t V; float *logits; int64_t ld; };
     template <int FM, int FN>
     static __device__ inline void run(const Args &a, f32x16 (&acc)[FM][FN], int64_t m, int64_t n, int, int64_t live) {
+        typedef __attribute__((ext_vector_type(4))) float f32x4;
         const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
-        const int64_t part = (a.first + m) / (32 * FM);
+        const int64_t part = ((STORE ? 0 : a.first) + m) / (32 * FM);
         const int v0 = (int)(a.first + m) + 4 * half, over = a.V - v0;         // entries from here on
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
@@ -122,6 +137,17 @@ struct LossStats {
                     acc[i][j][v] = at < over ? acc[i][j][v] : -INFINITY;
                 }
             if (y >= 0 && y < 32 * FM && (y & 4) == 0) a.hit[t] = hit;
+            if (STORE && t < live) {
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        f32x4 x;
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) x[u] = acc[i][j][4 * q + u];
+                        *(f32x4 *)(a.logits + t * a.ld + m + 32 * i + 8 * q + 4 * half) = x;
+                    }
+            }
             float top = acc[0][j][0];
 #pragma unroll
             for (int i = 0; i < FM; ++i)
@@ -140,8 +166,9 @@ struct LossStats {
     }
 };
 
-struct LossDelta {
-    struct Args { const int32_t *target; const float *lse, *nll, *weight; uint16_t *delta; int64_t Tp, ld, first; int32_t V; };
+// the second pass of dW: delta without the targets' entries, of a piece
+template <bool FEW> struct LossDelta {
+    struct Args { const int32_t *target; const float *lse, *weight; uint16_t *delta; int64_t ld, first; int32_t V; };
     template <int FM, int FN>
     static __device__ inline void run(const Args &a, f32x16 (&acc)[FM][FN], int64_t m, int64_t n, int, int64_t live) {
         const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
@@ -149,39 +176,43 @@ struct LossDelta {
         for (int j = 0; j < FN; ++j) {
             const int64_t t = n + 32 * j + l32;
             const bool on = t < live;
-            const float lse = on ? a.lse[t] : 0.0f, w = on ? a.weight[t] : 0.0f, at_target = on ? w * expm1f(-a.nll[t]) : 0.0f;
-            const int64_t y = on ? a.target[t] - a.first : -1;
+            const float lse = on ? a.lse[t] : 0.0f, w = on ? a.weight[t] : 0.0f;
+            const int c0 = (int)m + 4 * half, y = on ? a.target[t] - (int)a.first - c0 : -1, over = on ? a.V - (int)a.first - c0 : 0;
+            uint16_t *row = a.delta + t * a.ld + c0;
 #pragma unroll
             for (int i = 0; i < FM; ++i)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int64_t c = m + 32 * i + 8 * q + 4 * half;          // of the piece
-                    uint16_t d[4];
+                    uint16_t d[4], rest[4];
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
-                        float x = w * __expf(acc[i][j][4 * q + u] - lse);
-                        if (y == c + u) x = at_target;
-                        if (!on || a.first + c + u >= a.V) x = 0.0f;
+                        const int at = 32 * i + 8 * q + u;
+                        const float x = at < over && at != y ? w * __expf(acc[i][j][4 * q + u] - lse) : 0.0f;
                         d[u] = __builtin_bit_cast(uint16_t, (__bf16)x);
+                        rest[u] = __builtin_bit_cast(uint16_t, (__bf16)(x - __uint_as_float((uint32_t)d[u] << 16)));
                     }
-                    __builtin_memcpy(__builtin_assume_aligned(a.delta + t * a.ld + c, 8), d, 8);
+                    __builtin_memcpy(__builtin_assume_aligned(row + 32 * i + 8 * q, 8), d, 8);
+                    if (FEW) __builtin_memcpy(__builtin_assume_aligned(row + kFew * a.ld + 32 * i + 8 * q, 8), rest, 8);
                 }
         }
     }
 };
 
-// rows m are columns of dH, columns n tokens; pieces after the first add to what is there
-struct LossPlane {
-    struct Args { float *planes; int64_t Tp, Dp; int add; };
+// rows m are columns of dH, columns n tokens; pieces after the first add to what is there, shrunk.  FEW: columns kFew on are the second
+// terms of the first ones.
+template <bool FEW> struct LossPlane {
+    struct Args { float *planes; int64_t Tp, Dp; const float *shrink; };
     template <int FM, int FN>
     static __device__ inline void run(const Args &a, f32x16 (&acc)[FM][FN], int64_t m, int64_t n, int split, int64_t live) {
         typedef __attribute__((ext_vector_type(4))) float f32x4;
+        static_assert(!FEW || FN * 32 == 2 * kFew, "both terms in one wavefront");
         const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
+        for (int j = 0; j < (FEW ? 1 : FN); ++j) {
             const int64_t t = n + 32 * j + l32;
             if (t >= live) continue;
             float *row = a.planes + (split * a.Tp + t) * a.Dp;
+            const float shrink = a.shrink ? a.shrink[t] : 0.0f;
 #pragma unroll
             for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -190,20 +221,43 @@ struct LossPlane {
                     if (d >= a.Dp) continue;
                     f32x4 x;
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) x[u] = acc[i][j][4 * q + u];
-                    if (a.add) x += *(const f32x4 *)(row + d);
+                    for (int u = 0; u < 4; ++u) x[u] = FEW ? acc[i][0][4 * q + u] + acc[i][FN - 1][4 * q + u] : acc[i][j][4 * q + u];
+                    if (a.shrink) x += *(const f32x4 *)(row + d) * shrink;
                     *(f32x4 *)(row + d) = x;
                 }
         }
     }
 };
 
-// rows m are columns of dW, columns n vocabulary entries
+// rows m are columns of dW, columns n vocabulary entries; the targets' entries of delta are added here in fp32
 struct LossHead {
-    struct Args { uint16_t *dW; int64_t ld, first; int32_t V, D; };
+    struct Args {
+        uint16_t *dW; int64_t ld, first; int32_t V, D;
+        const int32_t *order, *order_target, *start; const float *pull; const uint16_t *H; int64_t Dp;
+    };
     template <int FM, int FN>
     static __device__ inline void run(const Args &a, f32x16 (&acc)[FM][FN], int64_t m, int64_t n, int, int64_t) {
+        static_assert(FN == 2, "64 entries a wavefront");
         const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
+        const int block = __builtin_amdgcn_readfirstlane((int)((a.first + n) / 64));
+        const int lo = a.start[block], hi = a.start[block + 1];
+        for (int x = lo; x < hi; ++x) {                    // in the order of target and token
+            const int r = __builtin_amdgcn_readfirstlane(a.order[x]), col = __builtin_amdgcn_readfirstlane(a.order_target[x]) & 63;
+            const float f = l32 == (col & 31) ? a.pull[r] : 0.0f;
+            const uint16_t *h = a.H + r * a.Dp + m + 4 * half;
+            auto add = [&](int j) {
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        uint16_t y[4] = {0, 0, 0, 0};
+                        if (m + 32 * i + 8 * q + 4 * half < a.Dp) __builtin_memcpy(y, __builtin_assume_aligned(h + 32 * i + 8 * q, 8), 8);
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) acc[i][j][4 * q + u] = __builtin_fmaf(f, __uint_as_float((uint32_t)y[u] << 16), acc[i][j][4 * q + u]);
+                    }
+            };
+            if (col < 32) add(0); else add(1);
+        }
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
             const int64_t v = a.first + n + 32 * j + l32;
@@ -226,7 +280,17 @@ struct LossHead {
     }
 };
 
-// lse and nll of TOK tokens from their parts, 256 / TOK threads each: the running maximum and the sum relative to it, then joined.
+// Maximum and sum (relative to it) of one token over parts p, p + lanes, ..; then of two such pairs.
+__device__ inline void join_pair(float &top, float &sum, float top2, float sum2) {
+    const float next = fmaxf(top, top2);
+    if (next == -INFINITY) sum += sum2;                     // 0, or NaN of logits that are not numbers
+    else sum = sum * __expf(top - next) + sum2 * __expf(top2 - next);
+    top = next;
+}
+// near 0 the loss keeps its digits
+__device__ inline float loss_of(float top, float sum, float hit) { return logf(sum) + (top - hit); }
+
+// lse and nll of TOK tokens from their parts, 256 / TOK threads each.
 template <int TOK>
 __global__ void __launch_bounds__(256)
 loss_join_kernel(LossTokens w, int64_t Tp, int64_t parts, float *nll, float *lse) {
@@ -239,36 +303,155 @@ loss_join_kernel(LossTokens w, int64_t Tp, int64_t parts, float *nll, float *lse
     float top = -INFINITY, sum = 0.0f;
     for (int64_t p = part; p < parts && t < live; p += LANES) {
         const float2 x = w.part[p * Tp + t];
-        const float next = fmaxf(top, x.x);
-        if (next == -INFINITY) sum += x.y;                  // 0, or NaN of logits that are not numbers
-        else sum = sum * __expf(top - next) + x.y * __expf(x.x - next);
-        top = next;
+        join_pair(top, sum, x.x, x.y);
     }
     s_top[threadIdx.x] = top; s_sum[threadIdx.x] = sum;
     __syncthreads();
     for (int h = LANES / 2; h > 0; h /= 2) {
         if (part < h) {
             const int o = threadIdx.x + h * TOK;
-            const float a = s_top[threadIdx.x], b = s_top[o], next = fmaxf(a, b);
-            if (next == -INFINITY) s_sum[threadIdx.x] += s_sum[o];
-            else s_sum[threadIdx.x] = s_sum[threadIdx.x] * __expf(a - next) + s_sum[o] * __expf(b - next);
-            s_top[threadIdx.x] = next;
+            join_pair(s_top[threadIdx.x], s_sum[threadIdx.x], s_top[o], s_sum[o]);
         }
         __syncthreads();
     }
     if (part == 0 && t < live) {
-        const float m = s_top[tok], l = logf(s_sum[tok]), all = m + l, one = l + (m - w.hit[t]);   // near 0 the loss keeps its digits
-        w.lse[t] = all; w.nll[t] = one;
+        const float all = s_top[tok] + logf(s_sum[tok]), one = loss_of(s_top[tok], s_sum[tok], w.hit[t]);
         const int64_t at = w.token[t];
+        w.lse[t] = all;
+        w.pull[t] = w.weight[t] * expm1f(-one);
         nll[at] = one;
         if (lse) lse[at] = all;
     }
 }
 
-// dH of a token: the sum of its planes, or zeros.
+// A token's logits of a piece become an operand of the products, without the target's entry.  Grid (tokens, shares of the row).
+//   RUN      p = exp(z - m), m the maximum so far; top, sum, shrink go on (one share)
+//   else     delta = w exp(z - lse), with its loss (the piece is the vocabulary)
+//   FEW      in two terms, rows t and t + kFew
+// Rows behind the live tokens, up to a whole stage, are zeros.
+template <bool RUN, bool FEW>
 __global__ void __launch_bounds__(256)
-loss_hidden_kernel(LossTokens w, int64_t Tp, int64_t Dp, int32_t D, int splits, uint16_t *dH, int64_t ld) {
+loss_delta_kernel(LossTokens w, int64_t Tp, int64_t parts, int64_t first, int64_t width, int64_t ld, float *nll, float *lse) {
+    __shared__ float s_top[4], s_sum[4];
+    const int64_t t = blockIdx.x, live = *w.count;
+    if (t >= (FEW ? kFew : (live + 63) / 64 * 64)) return;
+    const int tid = threadIdx.x;
+    const int64_t share = (width / 4 + gridDim.y - 1) / gridDim.y * 4, c0 = share * blockIdx.y, c1 = c0 + share < width ? c0 + share : width;
+    uint16_t *out = w.delta + t * ld;
+    auto put = [&](int64_t c, const float (&x)[4]) {
+        uint16_t d[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) d[u] = __builtin_bit_cast(uint16_t, (__bf16)x[u]);
+        __builtin_memcpy(__builtin_assume_aligned(out + c, 8), d, 8);
+        if (FEW) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) d[u] = __builtin_bit_cast(uint16_t, (__bf16)(x[u] - __uint_as_float((uint32_t)d[u] << 16)));
+            __builtin_memcpy(__builtin_assume_aligned(out + kFew * ld + c, 8), d, 8);
+        }
+    };
+    if (t >= live) {
+        const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int64_t c = c0 + 4 * tid; c < c1; c += 1024) put(c, zero);
+        return;
+    }
+    float top = -INFINITY, sum = 0.0f;
+    for (int64_t p = tid; p < parts; p += 256) {
+        const float2 x = w.part[p * Tp + t];
+        join_pair(top, sum, x.x, x.y);
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) {
+        const float o = __shfl_xor(top, d, 64), p = __shfl_xor(sum, d, 64);
+        join_pair(top, sum, o, p);
+    }
+    if ((tid & 63) == 0) { s_top[tid >> 6] = top; s_sum[tid >> 6] = sum; }
+    __syncthreads();
+    top = s_top[0]; sum = s_sum[0];
+#pragma unroll
+    for (int i = 1; i < 4; ++i) join_pair(top, sum, s_top[i], s_sum[i]);
+    float ref, scale = 1.0f;
+    if (RUN) {
+        const float before = first ? w.top[t] : -INFINITY, sum_before = first ? w.sum[t] : 0.0f;
+        __syncthreads();                                    // read before any thread writes it
+        join_pair(top, sum, before, sum_before);
+        ref = top;
+        if (tid == 0) { w.top[t] = top; w.sum[t] = sum; w.shrink[t] = __expf(before - top); }
+    } else {
+        ref = top + logf(sum);
+        scale = w.weight[t];
+        if (tid == 0 && blockIdx.y == 0) {
+            const float one = loss_of(top, sum, w.hit[t]);
+            const int64_t at = w.token[t];
+            w.pull[t] = scale * expm1f(-one);
+            nll[at] = one;
+            if (lse) lse[at] = ref;
+        }
+    }
+    const int64_t y = w.target[t] - first;
+    const float *z = w.logits + t * ld;
+    for (int64_t c = c0 + 4 * tid; c < c1; c += 1024) {
+        const float4 v = *(const float4 *)(z + c);
+        const float f[4] = {v.x, v.y, v.z, v.w};
+        float x[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[u] = c + u == y ? 0.0f : scale * __expf(f[u] - ref);
+        put(c, x);
+    }
+}
+
+// The live tokens in the order of target and token, and where each 64 vocabulary entries begin there: a thread counts what comes before
+// its token (or its 64 entries).  T (T + V / 64) comparisons, next to the 2 T D V operations of the products.
+__global__ void __launch_bounds__(256)
+loss_order_kernel(LossTokens w, int64_t T, int64_t blocks64) {
+    __shared__ int32_t s_target[1024];
+    const int live = *w.count;
+    const int64_t token_groups = (T + 255) / 256;
+    const bool by_token = blockIdx.x < token_groups;
+    const int64_t i = (by_token ? blockIdx.x : blockIdx.x - token_groups) * 256 + threadIdx.x;
+    if (by_token && (int64_t)blockIdx.x * 256 >= live) return;
+    const int mine = by_token ? (i < live ? w.target[i] : 0) : (int)(i * 64);
+    int before = 0;
+    for (int j0 = 0; j0 < live; j0 += 1024) {
+        __syncthreads();
+        for (int j = threadIdx.x; j < 1024; j += 256) s_target[j] = j0 + j < live ? w.target[j0 + j] : INT32_MAX;
+        __syncthreads();
+        const int left = by_token && i >= j0 ? (i - j0 < 1024 ? (int)(i - j0) : 1024) : 0;      // equal targets of earlier tokens
+        for (int j = 0; j < 1024; j += 4) {
+            const int4 y = *(const int4 *)(s_target + j);
+            before += (y.x < mine || (y.x == mine && j < left)) + (y.y < mine || (y.y == mine && j + 1 < left)) +
+                      (y.z < mine || (y.z == mine && j + 2 < left)) + (y.w < mine || (y.w == mine && j + 3 < left));
+        }
+    }
+    if (by_token) {
+        if (i < live) { w.order[before] = (int32_t)i; w.order_target[before] = mine; }
+    } else if (i < blocks64) {
+        w.start[i] = before;
+    }
+}
+
+// dH of a token: the sum of its planes (times w / s where they run), and the target's part; or zeros.
+__global__ void __launch_bounds__(256)
+loss_hidden_kernel(LossTokens w, int64_t Tp, int64_t Dp, int32_t D, int splits, int run, const uint16_t *W, int64_t ldW,
+                   uint16_t *dH, int64_t ld, float *nll, float *lse) {
     const int64_t t = blockIdx.x, r = w.place[t];
+    float scale = 1.0f, pull = 0.0f;
+    const uint16_t *row = W;
+    if (r >= 0) {
+        row += w.target[r] * ldW;
+        if (run) {
+            const float top = w.top[r], sum = w.sum[r], one = loss_of(top, sum, w.hit[r]), all = top + logf(sum);
+            scale = w.weight[r] / sum;
+            pull = w.weight[r] * expm1f(-one);
+            if (threadIdx.x == 0) {
+                nll[t] = one;
+                if (lse) lse[t] = all;
+                w.lse[r] = all;
+                w.pull[r] = pull;
+            }
+        } else {
+            pull = w.pull[r];
+        }
+    }
     for (int64_t c = threadIdx.x * 4; c < D; c += 256 * 4) {
         uint16_t x[4] = {0, 0, 0, 0};
         if (r >= 0) {
@@ -277,9 +460,14 @@ loss_hidden_kernel(LossTokens w, int64_t Tp, int64_t Dp, int32_t D, int splits, 
                 const float4 y = *(const float4 *)(w.planes + ((int64_t)p * Tp + r) * Dp + c);
                 s.x += y.x; s.y += y.y; s.z += y.z; s.w += y.w;
             }
+            uint16_t v[4] = {0, 0, 0, 0};
+            if (c + 4 <= D) __builtin_memcpy(v, row + c, 8);
+            else
+#pragma unroll
+                for (int u = 0; u < 4; ++u) if (c + u < D) v[u] = row[c + u];
             const float f[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
-            for (int u = 0; u < 4; ++u) x[u] = __builtin_bit_cast(uint16_t, (__bf16)f[u]);
+            for (int u = 0; u < 4; ++u) x[u] = __builtin_bit_cast(uint16_t, (__bf16)__builtin_fmaf(pull, __uint_as_float((uint32_t)v[u] << 16), scale * f[u]));
         }
         uint16_t *out = dH + t * ld + c;
         if (c + 4 <= D) __builtin_memcpy(out, x, 8);
@@ -289,26 +477,38 @@ loss_hidden_kernel(LossTokens w, int64_t Tp, int64_t Dp, int32_t D, int splits, 
     }
 }
 
-typedef ProductShape<256, 256, 2, 4, 2> LossWide;          // many tokens
-typedef ProductShape<256, 32, 8, 1, 4> LossFew;
+typedef ProductShape<256, 256, 2, 4, 2> Loss256;
+typedef ProductShape<256, 128, 4, 2, 3> Loss128;
+typedef ProductShape<256, 64, 8, 1, 4> Loss64;
+typedef ProductShape<256, 32, 8, 1, 4> Loss32;
 
 static int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 // Everything of a call that follows from its sizes.
-static LossPlan loss_plan(int64_t T, int32_t D, int32_t V, bool gradient) {
+static LossPlan loss_plan(int64_t T, int32_t D, int32_t V, bool want_dH, bool want_dW) {
     LossPlan p{};
     p.T = T; p.D = D; p.V = V;
-    p.tile_n = T <= 32 ? 32 : 256;
-    p.Tp = up_to(T > 0 ? T : 1, 256);
+    // the width of a tile of tokens that pads least, narrower ones a little dearer per token
+    p.tile_n = 256;
+    if (T <= 32) p.tile_n = 32;
+    else if (T <= 64) p.tile_n = 64;
+    else if (up_to(T, 128) * 11 < up_to(T, 256) * 10) p.tile_n = 128;
+    p.Tp = up_to(T > 0 ? T : 1, p.tile_n < 64 ? 64 : p.tile_n);
     p.Dp = up_to(D, 64);
     p.Vp = up_to(V, 256);
-    p.parts = p.Vp / 256 * (p.tile_n == 32 ? LossFew::WY : LossWide::WY);
-    // a piece: 256 MB of delta
-    int64_t Vc = ((int64_t)256 << 20) / (2 * p.Tp) / 256 * 256;
-    if (Vc < 256) Vc = 256;
-    if (Vc > p.Vp) Vc = p.Vp;
-    p.Vc = Vc;
-    const int64_t tiles = ((D + 255) / 256) * ((T + p.tile_n - 1) / p.tile_n), stages = Vc / 64;
+    p.parts = p.Vp / 32;                                    // at most (32 entries a part)
+    if (p.tile_n == 256) p.parts = p.Vp / 128;
+    if (p.tile_n == 128) p.parts = p.Vp / 64;
+    const bool gradient = want_dH || want_dW;
+    // A piece: the logits and delta of 200 MB stay in the last-level cache (256 MB).  With dW one piece of up to 1.5 GB saves the second pass,
+    // 2 T D V operations against 10 bytes a logit from memory.  Few tokens: one piece.
+    const int64_t rows = up_to(T > 0 ? T : 1, 64);
+    p.one_pass = T <= kFew || rows * p.Vp * 6 <= (want_dW ? (int64_t)1500 << 20 : (int64_t)200 << 20);
+    int64_t piece = p.one_pass ? p.Vp : ((int64_t)200 << 20) / (6 * p.Tp) / 256 * 256;
+    if (piece < 2048) piece = 2048;                         // a GEMM of K this long is worth its additions to the planes
+    if (piece > p.Vp) piece = p.Vp;
+    p.piece = piece;
+    const int64_t tiles = ((D + 255) / 256) * ((T + p.tile_n - 1) / p.tile_n), stages = piece / 64;
     int64_t splits = tiles > 0 ? 512 / tiles : 1;
     if (splits > stages / 8) splits = stages / 8;
     if (splits < 1) splits = 1;
@@ -316,32 +516,39 @@ static LossPlan loss_plan(int64_t T, int32_t D, int32_t V, bool gradient) {
     size_t at = 0;
     int i = 0;
     auto take = [&](size_t bytes) { p.off[i++] = at; at = (at + bytes + 255) & ~(size_t)255; };
-    take((size_t)p.Tp * p.Dp * 2);                          // H
-    take(256);                                              // count
-    take((size_t)p.Tp * 4); take((size_t)p.Tp * 4); take((size_t)p.Tp * 4);               // token, target, place
-    take((size_t)p.Tp * 4); take((size_t)p.Tp * 4); take((size_t)p.Tp * 4); take((size_t)p.Tp * 4);   // weight, lse, nll, hit
-    take((size_t)p.parts * p.Tp * 8);                       // part
-    // a piece's delta and, where W has to be packed, shorter pieces with the packed rows behind it: room for at least 64 MB of both
-    size_t piece = gradient ? (size_t)p.Tp * Vc * 2 : 0, both = (size_t)(p.Tp + p.Dp) * 2 * p.Vp;
-    if (both > ((size_t)64 << 20)) both = (size_t)64 << 20;
-    if (both < (size_t)(p.Tp + p.Dp) * 2 * 256) both = (size_t)(p.Tp + p.Dp) * 2 * 256;
-    take(piece > both ? piece : both);
-    take(gradient ? (size_t)p.splits * p.Tp * p.Dp * 4 : 0);
+    take((size_t)p.Tp * p.Dp * 2);                          // 0 H
+    take(256);                                              // 1 count
+    for (int j = 0; j < 10; ++j) take((size_t)p.Tp * 4);    // 2 token, target, place, weight, lse, hit, top, sum, shrink, pull
+    take((size_t)p.parts * p.Tp * 8);                       // 12 part
+    take(want_dW ? (size_t)p.Tp * 8 : 0);                   // 13 order, order_target
+    take(want_dW ? (size_t)(p.Vp / 64 + 1) * 4 : 0);        // 14 start
+    // 15: a piece's logits and delta; where W has to be packed, shorter pieces with the packed rows behind them: room for 64 MB of all three
+    const size_t each = (size_t)p.Tp * (gradient ? 6 : 0) + (size_t)p.Dp * 2;
+    size_t whole = gradient ? (size_t)p.Tp * piece * 6 : 0, packed = each * p.Vp;
+    if (packed > ((size_t)64 << 20)) packed = (size_t)64 << 20;
+    if (packed < each * 256) packed = each * 256;
+    take(whole > packed ? whole : packed);
+    take(want_dH ? (size_t)p.splits * p.Tp * p.Dp * 4 : 0); // 16 planes
     p.total = at;
     return p;
 }
 
 template <class Epilogue, int AK, int BK>
-static qless_status loss_product(const LossPlan &p, const ProductArgs &a, const typename Epilogue::Args &e, hipStream_t st) {
-    return p.tile_n == 32 ? launch_product<LossFew, AK, BK, Epilogue>(a, e, st) : launch_product<LossWide, AK, BK, Epilogue>(a, e, st);
+static qless_status loss_product(int tile_n, const ProductArgs &a, const typename Epilogue::Args &e, hipStream_t st) {
+    switch (tile_n) {
+        case 32: return launch_product<Loss32, AK, BK, Epilogue>(a, e, st);
+        case 64: return launch_product<Loss64, AK, BK, Epilogue>(a, e, st);
+        case 128: return launch_product<Loss128, AK, BK, Epilogue>(a, e, st);
+        default: return launch_product<Loss256, AK, BK, Epilogue>(a, e, st);
+    }
 }
 
 }  // namespace qless
 
-extern "C" size_t qless_token_loss_workspace(int64_t T, int32_t D, int32_t V, int gradient) {
+extern "C" size_t qless_token_loss_workspace(int64_t T, int32_t D, int32_t V, int want_dH, int want_dW) {
     using namespace qless;
     if (T < 0 || D < 1 || V < 1) return 0;
-    return loss_plan(T, D, V, gradient != 0).total;
+    return loss_plan(T, D, V, want_dH != 0, want_dW != 0).total;
 }
 
 extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void *W, int64_t ldW, qless_dtype dt, int64_t T, int32_t D, int32_t V,
@@ -352,65 +559,97 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
     if (dt != QLESS_BF16 || D > 65536 || T > 0x3FFFFFFF) return QLESS_ERR_UNSUPPORTED;
     if (T == 0 && !dW) return QLESS_OK;
     if (!W || (T > 0 && (!H || !target || !nll))) return QLESS_ERR_INVALID_ARG;
-    const bool gradient = dH || dW;
-    LossPlan p = loss_plan(T, D, V, gradient);
+    const LossPlan p = loss_plan(T, D, V, dH != nullptr, dW != nullptr);
     if (!ws || ws_bytes < p.total || ((uintptr_t)ws & 15) != 0) return QLESS_ERR_WORKSPACE;
     const qless_status ready = device_ready();
     if (ready != QLESS_OK) return ready;
     const hipStream_t st = (hipStream_t)stream;
     unsigned char *base = (unsigned char *)ws;
+    auto ints = [&](int i) { return (int32_t *)(base + p.off[i]); };
+    auto floats = [&](int i) { return (float *)(base + p.off[i]); };
     LossTokens w{};
-    w.H = (uint16_t *)(base + p.off[0]); w.count = (int32_t *)(base + p.off[1]);
-    w.token = (int32_t *)(base + p.off[2]); w.target = (int32_t *)(base + p.off[3]); w.place = (int32_t *)(base + p.off[4]);
-    w.weight = (float *)(base + p.off[5]); w.lse = (float *)(base + p.off[6]); w.nll = (float *)(base + p.off[7]); w.hit = (float *)(base + p.off[8]);
-    w.part = (float2 *)(base + p.off[9]); w.delta = (uint16_t *)(base + p.off[10]); w.planes = (float *)(base + p.off[11]);
-
-    hipLaunchKernelGGL(loss_live_kernel, dim3(1), dim3(kLossThreads), 0, st, target, weight, T, V, w, nll, lse);
-    hipLaunchKernelGGL(loss_rows_kernel, dim3((unsigned)p.Tp), dim3(256), 0, st, (const uint16_t *)H, ldH, D, w.token, w.count, p.Tp, w.H, p.Dp);
+    w.H = (uint16_t *)(base + p.off[0]); w.count = ints(1);
+    w.token = ints(2); w.target = ints(3); w.place = ints(4);
+    w.weight = floats(5); w.lse = floats(6); w.hit = floats(7); w.top = floats(8); w.sum = floats(9); w.shrink = floats(10); w.pull = floats(11);
+    w.part = (float2 *)(base + p.off[12]); w.order = ints(13); w.order_target = w.order + p.Tp; w.start = ints(14);
+    w.logits = floats(15); w.planes = floats(16);
 
     // W is read where it lies if its rows are whole 16-byte chunks; else a piece at a time is packed into the workspace
-    p.packed = ((uintptr_t)W & 15) != 0 || (ldW % 8 != 0 && V > 1) || D % 8 != 0 || ldW * 2 >= ((int64_t)1 << 23);
-    int64_t piece = p.Vc;
-    if (p.packed) {
-        piece = (int64_t)((p.off[11] - p.off[10]) / ((size_t)(p.Tp + p.Dp) * 2)) / 256 * 256;
-        if (piece > p.Vc) piece = p.Vc;
-        w.pack = w.delta + p.Tp * piece;
+    const bool packs = ((uintptr_t)W & 15) != 0 || (ldW % 8 != 0 && V > 1) || D % 8 != 0 || ldW * 2 >= ((int64_t)1 << 23);
+    const bool gradient = dH || dW, few = T <= kFew;
+    int64_t piece = gradient ? p.piece : p.Vp;
+    if (packs) {
+        const int64_t room = (int64_t)((p.off[16] - p.off[15]) / ((size_t)p.Tp * (gradient ? 6 : 0) + (size_t)p.Dp * 2)) / 256 * 256;
+        if (piece > room) piece = room;
     }
-    const ProductOperand tokens{w.H, p.Dp * 2, p.Tp, p.Dp * 2};
-    auto head = [&](int64_t v0, int64_t n) {               // n entries from v0 on, by rows of D
-        if (!p.packed) return ProductOperand{(const uint16_t *)W + v0 * ldW, ldW * 2, n, (int64_t)D * 2};
-        hipLaunchKernelGGL(loss_rows_kernel, dim3((unsigned)up_to(n, 256)), dim3(256), 0, st, (const uint16_t *)W + v0 * ldW, ldW, D, nullptr, nullptr, n, w.pack, p.Dp);
+    const bool one_pass = gradient && piece == p.Vp;
+    w.delta = (uint16_t *)(w.logits + p.Tp * piece);
+    w.pack = gradient ? w.delta + p.Tp * piece : (uint16_t *)w.logits;
+    auto rows_of = [&](int64_t v0) { return V - v0 < piece ? V - v0 : piece; };
+    auto head = [&](int64_t v0) {                           // a piece of W by rows of D
+        if (!packs) return ProductOperand{(const uint16_t *)W + v0 * ldW, V > 1 ? ldW * 2 : p.Dp * 2, rows_of(v0), (int64_t)D * 2};
+        const int64_t n = rows_of(v0);
+        hipLaunchKernelGGL(loss_rows_kernel, dim3((unsigned)up_to(n, 256)), dim3(256), 0, st, (const uint16_t *)W + v0 * ldW, ldW, D, nullptr, nullptr, n, 0, w.pack, p.Dp);
         return ProductOperand{w.pack, p.Dp * 2, n, p.Dp * 2};
     };
+    const ProductOperand tokens{w.H, p.Dp * 2, p.Tp, p.Dp * 2};
+    auto hidden_product = [&](const ProductOperand &rows, int64_t n, int64_t v0) {        // dH's planes: rows m columns of W, columns n tokens
+        ProductArgs a{ProductOperand{rows.base, rows.ld, rows.depth, n}, ProductOperand{w.delta, piece * 2, few ? 2 * kFew : p.Tp, up_to(n, 64) * 2},
+                      few ? 2 * kFew : T, n, few ? nullptr : w.count, nullptr, (D + 255) / 256, p.splits};
+        if (few) return launch_product<Loss64, ACROSS, ALONG, LossPlane<true>>(a, LossPlane<true>::Args{w.planes, p.Tp, p.Dp, v0 > 0 ? w.shrink : nullptr}, st);
+        return loss_product<LossPlane<false>, ACROSS, ALONG>(p.tile_n, a, LossPlane<false>::Args{w.planes, p.Tp, p.Dp, v0 > 0 ? w.shrink : nullptr}, st);
+    };
+    auto head_product = [&](int64_t n, int64_t v0) {        // dW: rows m columns of H, columns n entries
+        ProductArgs a{ProductOperand{w.H, p.Dp * 2, p.Dp * 2, p.Tp}, ProductOperand{w.delta, piece * 2, up_to(n, 64) * 2, few ? 2 * kFew : p.Tp},
+                      n, T == 0 ? 0 : few ? 2 * kFew : p.Tp, nullptr, few ? nullptr : w.count, (D + 255) / 256, 1};
+        return launch_product<Loss256, ACROSS, ACROSS, LossHead>(a, LossHead::Args{(uint16_t *)dW, ldDW, v0, V, D, w.order, w.order_target, w.start, w.pull, w.H, p.Dp}, st);
+    };
+
+    hipLaunchKernelGGL(loss_live_kernel, dim3(1), dim3(kLossThreads), 0, st, target, weight, T, V, w, nll, lse);
+    hipLaunchKernelGGL(loss_rows_kernel, dim3((unsigned)(few ? 2 * kFew : p.Tp)), dim3(256), 0, st, (const uint16_t *)H, ldH, D, w.token, w.count, p.Tp, few ? 1 : 0, w.H, p.Dp);
+    if (dW)
+        hipLaunchKernelGGL(loss_order_kernel, dim3((unsigned)((T + 255) / 256 + (p.Vp / 64 + 1 + 255) / 256)), dim3(256), 0, st, w, T, p.Vp / 64 + 1);
     qless_status rc = QLESS_OK;
-    if (T > 0) {
-        for (int64_t v0 = 0; v0 < V && rc == QLESS_OK; v0 += p.packed ? piece : p.Vp) {
-            const int64_t n = p.packed && V - v0 > piece ? piece : V - v0;
-            ProductArgs a{head(v0, n), tokens, T, p.Dp, w.count, nullptr, (int32_t)((n + 255) / 256), 1};
-            rc = loss_product<LossStats, ALONG, ALONG>(p, a, LossStats::Args{w.target, w.hit, w.part, p.Tp, v0, V}, st);
+    const int per_part = p.tile_n == 256 ? 128 : p.tile_n == 128 ? 64 : 32;
+
+    // first pass: the losses, and dH unless delta comes with dW
+    const bool run = dH && !one_pass;
+    for (int64_t v0 = 0; T > 0 && v0 < V && rc == QLESS_OK; v0 += piece) {
+        const int64_t n = rows_of(v0), np = up_to(n, 256);
+        const ProductOperand rows = head(v0);
+        const ProductArgs a{rows, tokens, T, p.Dp, w.count, nullptr, (int32_t)(np / 256), 1};
+        if (!dH && !one_pass) {
+            rc = loss_product<LossStats<false>, ALONG, ALONG>(p.tile_n, a, LossStats<false>::Args{w.target, w.hit, w.part, p.Tp, v0, V, nullptr, 0}, st);
+            continue;
         }
-        if (rc != QLESS_OK) return rc;
-        if (T <= 64) hipLaunchKernelGGL(loss_join_kernel<1>, dim3((unsigned)T), dim3(256), 0, st, w, p.Tp, p.parts, nll, lse);
-        else hipLaunchKernelGGL(loss_join_kernel<16>, dim3((unsigned)((T + 15) / 16)), dim3(256), 0, st, w, p.Tp, p.parts, nll, lse);
-    }
-    for (int64_t v0 = 0; gradient && v0 < V && rc == QLESS_OK; v0 += piece) {
-        const int64_t n = V - v0 < piece ? V - v0 : piece, np = up_to(n, 256);
-        const ProductOperand rows = head(v0, n);
-        ProductArgs a{rows, tokens, T, p.Dp, w.count, nullptr, (int32_t)(np / 256), 1};
-        rc = loss_product<LossDelta, ALONG, ALONG>(p, a, LossDelta::Args{w.target, w.lse, w.nll, w.weight, w.delta, p.Tp, piece, v0, V}, st);
-        if (rc == QLESS_OK && dH) {
-            ProductArgs b{ProductOperand{rows.base, rows.ld, rows.depth, n}, ProductOperand{w.delta, piece * 2, p.Tp, np * 2}, T, n, w.count, nullptr,
-                          (D + 255) / 256, p.splits};
-            rc = loss_product<LossPlane, ACROSS, ALONG>(p, b, LossPlane::Args{w.planes, p.Tp, p.Dp, v0 > 0}, st);
-        }
-        if (rc == QLESS_OK && dW) {
-            ProductArgs b{ProductOperand{w.H, p.Dp * 2, p.Dp * 2, p.Tp}, ProductOperand{w.delta, piece * 2, np * 2, up_to(T > 0 ? T : 1, p.tile_n)}, n, p.Tp, nullptr, w.count,
-                          (D + 255) / 256, 1};
-            rc = launch_product<LossWide, ACROSS, ACROSS, LossHead>(b, LossHead::Args{(uint16_t *)dW, ldDW, v0, V, D}, st);
-        }
+        rc = loss_product<LossStats<true>, ALONG, ALONG>(p.tile_n, a, LossStats<true>::Args{w.target, w.hit, w.part, p.Tp, v0, V, w.logits, piece}, st);
+        if (rc != QLESS_OK) break;
+        int64_t shares = run || T >= 1024 ? 1 : 1024 / T + 1;                  // of a row
+        if (shares > np / 1024) shares = np / 1024 > 0 ? np / 1024 : 1;
+        const dim3 grid((unsigned)up_to(T, few ? kFew : 64), (unsigned)shares);
+        const int64_t parts = np / per_part;
+        auto delta = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, w, p.Tp, parts, v0, np, piece, nll, lse); };
+        if (run) few ? delta(loss_delta_kernel<true, true>) : delta(loss_delta_kernel<true, false>);
+        else few ? delta(loss_delta_kernel<false, true>) : delta(loss_delta_kernel<false, false>);
+        if (dH) rc = hidden_product(rows, n, v0);
+        if (rc == QLESS_OK && dW && one_pass) rc = head_product(n, v0);
     }
     if (rc != QLESS_OK) return rc;
-    if (dH && T > 0)
-        hipLaunchKernelGGL(loss_hidden_kernel, dim3((unsigned)T), dim3(256), 0, st, w, p.Tp, p.Dp, D, p.splits, (uint16_t *)dH, ldDH);
-    return launch_status();
+    if (T > 0 && !dH && !one_pass) {
+        const int64_t parts = p.Vp / per_part;
+        if (T <= 64) hipLaunchKernelGGL(loss_join_kernel<1>, dim3((unsigned)T), dim3(256), 0, st, w, p.Tp, parts, nll, lse);
+        else hipLaunchKernelGGL(loss_join_kernel<16>, dim3((unsigned)((T + 15) / 16)), dim3(256), 0, st, w, p.Tp, parts, nll, lse);
+    }
+    if (T > 0 && dH)
+        hipLaunchKernelGGL(loss_hidden_kernel, dim3((unsigned)T), dim3(256), 0, st, w, p.Tp, p.Dp, D, p.splits, run ? 1 : 0, (const uint16_t *)W, ldW, (uint16_t *)dH, ldDH, nll, lse);
+
+    // second pass: delta from the known losses, a piece at a time, and dW
+    for (int64_t v0 = 0; dW && (!one_pass || T == 0) && v0 < V && rc == QLESS_OK; v0 += piece) {
+        const int64_t n = rows_of(v0);
+        const ProductArgs a{head(v0), tokens, T, p.Dp, w.count, nullptr, (int32_t)(up_to(n, 256) / 256), 1};
+        if (few) rc = launch_product<Loss32, ALONG, ALONG, LossDelta<true>>(a, LossDelta<true>::Args{w.target, w.lse, w.weight, w.delta, piece, v0, V}, st);
+        else rc = loss_product<LossDelta<false>, ALONG, ALONG>(p.tile_n, a, LossDelta<false>::Args{w.target, w.lse, w.weight, w.delta, piece, v0, V}, st);
+        if (rc == QLESS_OK) rc = head_product(n, v0);
+    }
+    return rc == QLESS_OK ? launch_status() : rc;
 }

@@ -18,16 +18,16 @@ def test_refusals():
         assert call(**bad) == INVALID, bad
     for bad in (dict(dt=0), dict(dt=2), dict(D=65537, ldH=65537, ldW=65537, ldDH=65537, ldDW=65537), dict(T=1 << 30)):
         assert call(**bad) == UNSUPPORTED, bad
-    need = L.qless_token_loss_workspace(4, 64, 100, 1)
-    assert need > L.qless_token_loss_workspace(4, 64, 100, 0) > 0
+    need = L.qless_token_loss_workspace(4, 64, 100, 1, 1)
+    assert need > L.qless_token_loss_workspace(4, 64, 100, 1, 0) > L.qless_token_loss_workspace(4, 64, 100, 0, 0) > 0
     for bad in (dict(wsb=need - 1), dict(ws=None), dict(ws=ctypes.c_void_p(24))):
         assert call(**bad) == WORKSPACE, bad
     assert call(T=0, dW=None, H=None, target=None, nll=None, ws=None, wsb=0) == OK
-    for shape in ((-1, 64, 100, 1), (4, 0, 100, 1), (4, 64, 0, 1)):
+    for shape in ((-1, 64, 100, 1, 1), (4, 0, 100, 1, 1), (4, 64, 0, 1, 1)):
         assert L.qless_token_loss_workspace(*shape) == 0
 
 
 def test_workspace_does_not_hold_the_logits():
     L = binding.lib()
     T, D, V = 65536, 4096, 131072
-    assert L.qless_token_loss_workspace(T, D, V, 1) < T * V * 2 // 4
+    assert L.qless_token_loss_workspace(T, D, V, 1, 1) < T * V * 2 // 4
