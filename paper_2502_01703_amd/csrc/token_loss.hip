@@ -45,63 +45,89 @@ constexpr int kFew = 32;                   // tokens up to which the rest of del
 
 constexpr int kLossThreads = 1024;
 
-// One workgroup numbers the live tokens in their order: eight tokens a thread and pass.
+// The live tokens numbered in their order: a workgroup a thousand tokens, whose place follows from a count of the targets before them.
 __global__ void __launch_bounds__(kLossThreads)
 loss_live_kernel(const int64_t *target, const float *weight, int64_t T, int32_t V, LossTokens w, float *nll, float *lse) {
-    __shared__ int32_t s_wave[kLossThreads / 64];
+    __shared__ int32_t s_before[kLossThreads / 64], s_wave[kLossThreads / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int32_t before = 0;
-    for (int64_t t0 = 0; t0 < T; t0 += 8 * kLossThreads) {
-        int64_t y[8];
-        int32_t mine = 0;
+    const int64_t t0 = (int64_t)blockIdx.x * kLossThreads, t = t0 + tid;
+    int32_t earlier = 0;
+    for (int64_t i = tid; i < t0; i += kLossThreads) {
+        const int64_t y = target[i];
+        earlier += y >= 0 && y < V;
+    }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int64_t t = t0 + 8 * tid + i;
-            y[i] = t < T ? target[t] : -1;
-            mine += y[i] >= 0 && y[i] < V;
-        }
-        int32_t up = mine;                                 // inclusive sums over the wavefront
+    for (int d = 32; d > 0; d /= 2) earlier += __shfl_xor(earlier, d, 64);
+    const int64_t y = t < T ? target[t] : -1;
+    const bool live = y >= 0 && y < V;
+    const uint64_t votes = __ballot(live);
+    if (lane == 0) { s_before[wave] = earlier; s_wave[wave] = __popcll(votes); }
+    __syncthreads();
+    int32_t at = __popcll(votes & (((uint64_t)1 << lane) - 1)), all = 0;
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int32_t o = __shfl_up(up, d, 64);
-            up += lane >= d ? o : 0;
-        }
-        __syncthreads();
-        if (lane == 63) s_wave[wave] = up;
-        __syncthreads();
-        int32_t at = before + up - mine;
-        for (int i = 0; i < kLossThreads / 64; ++i) {
-            if (i < wave) at += s_wave[i];
-            before += s_wave[i];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int64_t t = t0 + 8 * tid + i;
-            if (t >= T) break;
-            const bool live = y[i] >= 0 && y[i] < V;
-            w.place[t] = live ? at : -1;
-            if (live) {
-                w.token[at] = (int32_t)t;
-                w.target[at] = (int32_t)y[i];
-                w.weight[at] = weight ? weight[t] : 1.0f;
-                ++at;
-            } else {
-                nll[t] = 0.0f;
-                if (lse) lse[t] = 0.0f;
-            }
+    for (int i = 0; i < kLossThreads / 64; ++i) {
+        at += s_before[i] + (i < wave ? s_wave[i] : 0);
+        all += s_before[i] + s_wave[i];
+    }
+    if (t < T) {
+        w.place[t] = live ? at : -1;
+        if (live) {
+            w.token[at] = (int32_t)t;
+            w.target[at] = (int32_t)y;
+            w.weight[at] = weight ? weight[t] : 1.0f;
+        } else {
+            nll[t] = 0.0f;
+            if (lse) lse[t] = 0.0f;
         }
     }
-    if (tid == 0) *w.count = before;
+    if (tid == 0 && t0 + kLossThreads >= T) *w.count = all;
+}
+
+// The same for at most 64 tokens, together with the rows of H: a workgroup a row of the gathered ones.
+__global__ void __launch_bounds__(256)
+loss_start_kernel(const int64_t *target, const float *weight, int T, int32_t V, LossTokens w, float *nll, float *lse,
+                  const uint16_t *H, int64_t ldH, int32_t D, int64_t Dp, int few) {
+    const int lane = threadIdx.x & 63, r = blockIdx.x, of = few && r >= kFew ? r - kFew : r;
+    const int64_t y = lane < T ? target[lane] : -1;
+    const bool live = y >= 0 && y < V;
+    const uint64_t votes = __ballot(live);
+    const int at = __popcll(votes & (((uint64_t)1 << lane) - 1)), count = __popcll(votes);
+    if (r == 0 && threadIdx.x < 64) {
+        if (lane < T) {
+            w.place[lane] = live ? at : -1;
+            if (live) {
+                w.token[at] = lane;
+                w.target[at] = (int32_t)y;
+                w.weight[at] = weight ? weight[lane] : 1.0f;
+            } else {
+                nll[lane] = 0.0f;
+                if (lse) lse[lane] = 0.0f;
+            }
+        }
+        if (lane == 0) *w.count = count;
+    }
+    const int from = of < count ? __ffsll((unsigned long long)__ballot(live && at == of)) - 1 : 0;
+    for (int64_t c = threadIdx.x * 8; c < Dp; c += 256 * 8) {
+        uint16_t v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 0;
+        const uint16_t *x = H + from * ldH + c;
+        if (of < count && c + 8 <= D) __builtin_memcpy(v, x, 16);
+        else if (of < count)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) if (c + i < D) v[i] = x[i];
+        __builtin_memcpy(__builtin_assume_aligned(w.H + r * Dp + c, 16), v, 16);
+    }
 }
 
 // Rows of bfloat16 copied to rows of ld (a multiple of 64) with zeros behind their D elements, eight elements a thread; `from` null: row r,
-// else the row that it names, and zeros from *count up to whole tiles; few: rows from kFew on repeat the first ones.
+// else the row that it names, and zeros from *count up to whole tiles.
 __global__ void __launch_bounds__(256)
-loss_rows_kernel(const uint16_t *X, int64_t ldX, int32_t D, const int32_t *from, const int32_t *count, int64_t rows, int few, uint16_t *out, int64_t ld) {
-    const int64_t r = blockIdx.x, of = few && r >= kFew ? r - kFew : r;
+loss_rows_kernel(const uint16_t *X, int64_t ldX, int32_t D, const int32_t *from, const int32_t *count, int64_t rows, uint16_t *out, int64_t ld) {
+    const int64_t r = blockIdx.x;
     const int64_t n = count ? *count : rows;
-    if (r >= (n + 255) / 256 * 256 && !few) return;
-    const uint16_t *x = of < n ? X + (from ? (int64_t)from[of] : of) * ldX : nullptr;
+    if (r >= (n + 255) / 256 * 256) return;
+    const uint16_t *x = r < n ? X + (from ? (int64_t)from[r] : r) * ldX : nullptr;
     for (int64_t c = threadIdx.x * 8; c < ld; c += 256 * 8) {
         uint16_t v[8];
 #pragma unroll
@@ -399,50 +425,49 @@ loss_delta_kernel(LossTokens w, int64_t Tp, int64_t parts, int64_t first, int64_
     }
 }
 
-// The live tokens in the order of target and token, and where each 64 vocabulary entries begin there: a thread counts what comes before
-// its token (or its 64 entries).  T (T + V / 64) comparisons, next to the 2 T D V operations of the products.
+// The live tokens in the order of target and token, and where each 64 vocabulary entries begin there: 16 threads count what comes before
+// a token (or before 64 entries).  T (T + V / 64) comparisons, next to the 2 T D V operations of the products.
 __global__ void __launch_bounds__(256)
 loss_order_kernel(LossTokens w, int64_t T, int64_t blocks64) {
-    __shared__ int32_t s_target[1024];
-    const int live = *w.count;
-    const int64_t token_groups = (T + 255) / 256;
+    const int live = *w.count, sub = threadIdx.x & 15;
+    const int64_t token_groups = (T + 15) / 16;
     const bool by_token = blockIdx.x < token_groups;
-    const int64_t i = (by_token ? blockIdx.x : blockIdx.x - token_groups) * 256 + threadIdx.x;
-    if (by_token && (int64_t)blockIdx.x * 256 >= live) return;
-    const int mine = by_token ? (i < live ? w.target[i] : 0) : (int)(i * 64);
+    const int64_t i = (by_token ? blockIdx.x : blockIdx.x - token_groups) * 16 + (threadIdx.x >> 4);
+    if (by_token ? i >= live : i >= blocks64) return;      // whole rows of 16 lanes
+    const int mine = by_token ? w.target[i] : (int)(i * 64);
     int before = 0;
-    for (int j0 = 0; j0 < live; j0 += 1024) {
-        __syncthreads();
-        for (int j = threadIdx.x; j < 1024; j += 256) s_target[j] = j0 + j < live ? w.target[j0 + j] : INT32_MAX;
-        __syncthreads();
-        const int left = by_token && i >= j0 ? (i - j0 < 1024 ? (int)(i - j0) : 1024) : 0;      // equal targets of earlier tokens
-        for (int j = 0; j < 1024; j += 4) {
-            const int4 y = *(const int4 *)(s_target + j);
-            before += (y.x < mine || (y.x == mine && j < left)) + (y.y < mine || (y.y == mine && j + 1 < left)) +
-                      (y.z < mine || (y.z == mine && j + 2 < left)) + (y.w < mine || (y.w == mine && j + 3 < left));
-        }
+#pragma unroll 8
+    for (int j = sub; j < live; j += 16) {
+        const int y = w.target[j];
+        before += y < mine || (by_token && y == mine && j < i);
     }
-    if (by_token) {
-        if (i < live) { w.order[before] = (int32_t)i; w.order_target[before] = mine; }
-    } else if (i < blocks64) {
-        w.start[i] = before;
-    }
+#pragma unroll
+    for (int d = 8; d > 0; d /= 2) before += __shfl_xor(before, d, 16);
+    if (sub != 0) return;
+    if (by_token) { w.order[before] = (int32_t)i; w.order_target[before] = mine; }
+    else w.start[i] = before;
 }
 
-// dH of a token: the sum of its planes (times w / s where they run), and the target's part; or zeros.
+// dH of a token: the sum of its planes (times w / s where they run), and the target's part; or zeros.  SG threads share the planes
+// of four columns, in a fixed order.
+template <int SG>
 __global__ void __launch_bounds__(256)
 loss_hidden_kernel(LossTokens w, int64_t Tp, int64_t Dp, int32_t D, int splits, int run, const uint16_t *W, int64_t ldW,
                    uint16_t *dH, int64_t ld, float *nll, float *lse) {
+    constexpr int COLS = 256 / SG;
+    __shared__ float4 s_sum[SG > 1 ? 256 : 1];
     const int64_t t = blockIdx.x, r = w.place[t];
+    const int col = threadIdx.x % COLS, sg = threadIdx.x / COLS;
     float scale = 1.0f, pull = 0.0f;
     const uint16_t *row = W;
     if (r >= 0) {
         row += w.target[r] * ldW;
         if (run) {
-            const float top = w.top[r], sum = w.sum[r], one = loss_of(top, sum, w.hit[r]), all = top + logf(sum);
+            const float top = w.top[r], sum = w.sum[r], one = loss_of(top, sum, w.hit[r]);
             scale = w.weight[r] / sum;
             pull = w.weight[r] * expm1f(-one);
-            if (threadIdx.x == 0) {
+            if (threadIdx.x == 0 && blockIdx.y == 0) {
+                const float all = top + logf(sum);
                 nll[t] = one;
                 if (lse) lse[t] = all;
                 w.lse[r] = all;
@@ -452,14 +477,30 @@ loss_hidden_kernel(LossTokens w, int64_t Tp, int64_t Dp, int32_t D, int splits, 
             pull = w.pull[r];
         }
     }
-    for (int64_t c = threadIdx.x * 4; c < D; c += 256 * 4) {
-        uint16_t x[4] = {0, 0, 0, 0};
-        if (r >= 0) {
-            float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            for (int p = 0; p < splits; ++p) {
+    for (int64_t c0 = (int64_t)blockIdx.y * COLS * 4; c0 < D; c0 += (int64_t)gridDim.y * COLS * 4) {     // the same for the workgroup
+        const int64_t c = c0 + col * 4;
+        float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (r >= 0 && c < D) {
+#pragma unroll 4
+            for (int p = sg; p < splits; p += SG) {
                 const float4 y = *(const float4 *)(w.planes + ((int64_t)p * Tp + r) * Dp + c);
                 s.x += y.x; s.y += y.y; s.z += y.z; s.w += y.w;
             }
+        }
+        if (SG > 1) {
+            s_sum[threadIdx.x] = s;
+            __syncthreads();
+            if (sg == 0)
+#pragma unroll
+                for (int g = 1; g < SG; ++g) {
+                    const float4 y = s_sum[g * COLS + col];
+                    s.x += y.x; s.y += y.y; s.z += y.z; s.w += y.w;
+                }
+            __syncthreads();
+        }
+        if (sg != 0 || c >= D) continue;
+        uint16_t x[4] = {0, 0, 0, 0};
+        if (r >= 0) {
             uint16_t v[4] = {0, 0, 0, 0};
             if (c + 4 <= D) __builtin_memcpy(v, row + c, 8);
             else
@@ -488,11 +529,7 @@ static int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 static LossPlan loss_plan(int64_t T, int32_t D, int32_t V, bool want_dH, bool want_dW) {
     LossPlan p{};
     p.T = T; p.D = D; p.V = V;
-    // the width of a tile of tokens that pads least, narrower ones a little dearer per token
-    p.tile_n = 256;
-    if (T <= 32) p.tile_n = 32;
-    else if (T <= 64) p.tile_n = 64;
-    else if (up_to(T, 128) * 11 < up_to(T, 256) * 10) p.tile_n = 128;
+    p.tile_n = T <= 32 ? 32 : T <= 64 ? 64 : T <= 128 ? 128 : 256;
     p.Tp = up_to(T > 0 ? T : 1, p.tile_n < 64 ? 64 : p.tile_n);
     p.Dp = up_to(D, 64);
     p.Vp = up_to(V, 256);
@@ -500,16 +537,24 @@ static LossPlan loss_plan(int64_t T, int32_t D, int32_t V, bool want_dH, bool wa
     if (p.tile_n == 256) p.parts = p.Vp / 128;
     if (p.tile_n == 128) p.parts = p.Vp / 64;
     const bool gradient = want_dH || want_dW;
-    // A piece: the logits and delta of 200 MB stay in the last-level cache (256 MB).  With dW one piece of up to 1.5 GB saves the second pass,
-    // 2 T D V operations against 10 bytes a logit from memory.  Few tokens: one piece.
-    const int64_t rows = up_to(T > 0 ? T : 1, 64);
-    p.one_pass = T <= kFew || rows * p.Vp * 6 <= (want_dW ? (int64_t)1500 << 20 : (int64_t)200 << 20);
-    int64_t piece = p.one_pass ? p.Vp : ((int64_t)200 << 20) / (6 * p.Tp) / 256 * 256;
-    if (piece < 2048) piece = 2048;                         // a GEMM of K this long is worth its additions to the planes
-    if (piece > p.Vp) piece = p.Vp;
+    // A piece: logits and delta of up to 768 MB.  (Their 10 bytes a logit come from memory at any size that is worth its additions to
+    // the planes.)  With dW one piece of up to 1.5 GB saves the second pass.  Few tokens: one piece.
+    const int64_t budget = (int64_t)(want_dW ? 1536 : 768) << 20, cus = compute_units();
+    const int64_t ntiles = (T + p.tile_n - 1) / p.tile_n;
+    p.one_pass = T <= kFew || p.Tp * p.Vp * 6 <= budget;
+    int64_t piece = p.Vp;
+    if (!p.one_pass) {
+        // whole rounds of tiles of the chip, if all tokens are live
+        int64_t m = ((int64_t)768 << 20) / (6 * p.Tp) / 256;
+        if (m < 8) m = 8;
+        const int64_t rounds = m * ntiles / cus;
+        if (rounds > 0) m = rounds * cus / ntiles > 0 ? rounds * cus / ntiles : 1;
+        piece = m * 256;
+        if (piece > p.Vp) piece = p.Vp;
+    }
     p.piece = piece;
-    const int64_t tiles = ((D + 255) / 256) * ((T + p.tile_n - 1) / p.tile_n), stages = piece / 64;
-    int64_t splits = tiles > 0 ? 512 / tiles : 1;
+    const int64_t tiles = ((D + 255) / 256) * ntiles, stages = piece / 64;
+    int64_t splits = tiles > 0 ? 2 * cus / tiles : 1;
     if (splits > stages / 8) splits = stages / 8;
     if (splits < 1) splits = 1;
     p.splits = (int32_t)splits;
@@ -589,7 +634,7 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
     auto head = [&](int64_t v0) {                           // a piece of W by rows of D
         if (!packs) return ProductOperand{(const uint16_t *)W + v0 * ldW, V > 1 ? ldW * 2 : p.Dp * 2, rows_of(v0), (int64_t)D * 2};
         const int64_t n = rows_of(v0);
-        hipLaunchKernelGGL(loss_rows_kernel, dim3((unsigned)up_to(n, 256)), dim3(256), 0, st, (const uint16_t *)W + v0 * ldW, ldW, D, nullptr, nullptr, n, 0, w.pack, p.Dp);
+        hipLaunchKernelGGL(loss_rows_kernel, dim3((unsigned)up_to(n, 256)), dim3(256), 0, st, (const uint16_t *)W + v0 * ldW, ldW, D, nullptr, nullptr, n, w.pack, p.Dp);
         return ProductOperand{w.pack, p.Dp * 2, n, p.Dp * 2};
     };
     const ProductOperand tokens{w.H, p.Dp * 2, p.Tp, p.Dp * 2};
@@ -605,10 +650,14 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
         return launch_product<Loss256, ACROSS, ACROSS, LossHead>(a, LossHead::Args{(uint16_t *)dW, ldDW, v0, V, D, w.order, w.order_target, w.start, w.pull, w.H, p.Dp}, st);
     };
 
-    hipLaunchKernelGGL(loss_live_kernel, dim3(1), dim3(kLossThreads), 0, st, target, weight, T, V, w, nll, lse);
-    hipLaunchKernelGGL(loss_rows_kernel, dim3((unsigned)(few ? 2 * kFew : p.Tp)), dim3(256), 0, st, (const uint16_t *)H, ldH, D, w.token, w.count, p.Tp, few ? 1 : 0, w.H, p.Dp);
+    if (T <= 64) {
+        hipLaunchKernelGGL(loss_start_kernel, dim3((unsigned)p.Tp), dim3(256), 0, st, target, weight, (int)T, V, w, nll, lse, (const uint16_t *)H, ldH, D, p.Dp, few ? 1 : 0);
+    } else {
+        hipLaunchKernelGGL(loss_live_kernel, dim3((unsigned)((T + kLossThreads - 1) / kLossThreads)), dim3(kLossThreads), 0, st, target, weight, T, V, w, nll, lse);
+        hipLaunchKernelGGL(loss_rows_kernel, dim3((unsigned)p.Tp), dim3(256), 0, st, (const uint16_t *)H, ldH, D, w.token, w.count, p.Tp, w.H, p.Dp);
+    }
     if (dW)
-        hipLaunchKernelGGL(loss_order_kernel, dim3((unsigned)((T + 255) / 256 + (p.Vp / 64 + 1 + 255) / 256)), dim3(256), 0, st, w, T, p.Vp / 64 + 1);
+        hipLaunchKernelGGL(loss_order_kernel, dim3((unsigned)((T + 15) / 16 + (p.Vp / 64 + 1 + 15) / 16)), dim3(256), 0, st, w, T, p.Vp / 64 + 1);
     qless_status rc = QLESS_OK;
     const int per_part = p.tile_n == 256 ? 128 : p.tile_n == 128 ? 64 : 32;
 
@@ -638,10 +687,18 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
     if (T > 0 && !dH && !one_pass) {
         const int64_t parts = p.Vp / per_part;
         if (T <= 64) hipLaunchKernelGGL(loss_join_kernel<1>, dim3((unsigned)T), dim3(256), 0, st, w, p.Tp, parts, nll, lse);
-        else hipLaunchKernelGGL(loss_join_kernel<16>, dim3((unsigned)((T + 15) / 16)), dim3(256), 0, st, w, p.Tp, parts, nll, lse);
+        else hipLaunchKernelGGL(loss_join_kernel<4>, dim3((unsigned)((T + 3) / 4)), dim3(256), 0, st, w, p.Tp, parts, nll, lse);
     }
-    if (T > 0 && dH)
-        hipLaunchKernelGGL(loss_hidden_kernel, dim3((unsigned)T), dim3(256), 0, st, w, p.Tp, p.Dp, D, p.splits, run ? 1 : 0, (const uint16_t *)W, ldW, (uint16_t *)dH, ldDH, nll, lse);
+    if (T > 0 && dH) {
+        auto hidden = [&](auto kernel, int cols) {
+            int64_t shares = 2048 / T + 1;
+            if (shares > (D + cols - 1) / cols) shares = (D + cols - 1) / cols;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)T, (unsigned)shares), dim3(256), 0, st, w, p.Tp, p.Dp, D, p.splits, run ? 1 : 0, (const uint16_t *)W, ldW, (uint16_t *)dH, ldDH, nll, lse);
+        };
+        if (p.splits >= 16) hidden(loss_hidden_kernel<16>, 64);
+        else if (p.splits >= 4) hidden(loss_hidden_kernel<4>, 256);
+        else hidden(loss_hidden_kernel<1>, 1024);
+    }
 
     // second pass: delta from the known losses, a piece at a time, and dW
     for (int64_t v0 = 0; dW && (!one_pass || T == 0) && v0 < V && rc == QLESS_OK; v0 += piece) {
