@@ -132,13 +132,12 @@ product_kernel(ProductArgs p, typename Epilogue::Args e) {
     constexpr int UA = ProductCopies<AK, Sh::MT, NW>::U, UB = ProductCopies<BK, Sh::NT, NW>::U;
     ca.init(p.a, m0, lane, wave);
     cb.init(p.b, n0, lane, wave);
-    auto request = [&](int s, int slot) {
-        if (s > s1 - 1) s = s1 - 1;                        // repeated past the end: all stages count alike
+    constexpr int U = UA + UB;
+    auto request = [&](int u, int s, int slot) {           // copy u of a stage; past the end the last one again: all stages count alike
+        if (s > s1 - 1) s = s1 - 1;
         const unsigned at = lds0 + (unsigned)(slot * Sh::STAGE);
-#pragma unroll
-        for (int u = 0; u < UA; ++u) ca.issue(u, s, lane, wave, at);
-#pragma unroll
-        for (int u = 0; u < UB; ++u) cb.issue(u, s, lane, wave, at + Sh::MT * 128);
+        if (u < UA) ca.issue(u, s, lane, wave, at);
+        else cb.issue(u - UA, s, lane, wave, at + Sh::MT * 128);
     };
     f32x16 acc[FM][FN];
 #pragma unroll
@@ -150,29 +149,56 @@ product_kernel(ProductArgs p, typename Epilogue::Args e) {
     const unsigned la = fragment_lane<AK, Sh::MT>(lane), lb = fragment_lane<BK, Sh::NT>(lane);
     const int ma = wy * FM * 32, nb = wx * FN * 32;
     if (s0 < s1) {
+        bf16x8 fa[2][FM], fb[2][FN];
+        auto read = [&](int set, int f, int slot, int kk) {          // fragment f of a K step of 16: the columns', then the rows'
+            const unsigned char *sa = smem + slot * Sh::STAGE;
+            if (f < FN) fb[set][f] = fragment<BK, Sh::NT>(sa + Sh::MT * 128, lb, nb + 32 * f, kk);
+            else fa[set][f - FN] = fragment<AK, Sh::MT>(sa, la, ma + 32 * (f - FN), kk);
+        };
+        auto pin = []() { __builtin_amdgcn_sched_barrier(0); };      // keeps the order below
 #pragma unroll
-        for (int i = 0; i < NS - 1; ++i) request(s0 + i, i);
+        for (int i = 0; i < NS; ++i)
+#pragma unroll
+            for (int u = 0; u < U; ++u) request(u, s0 + i, i);
+        wait_vmcnt<(NS - 1) * U>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int f = 0; f < FM + FN; ++f) read(0, f, 0, 0);
         int slot = 0;
+        // The fragments of a K step are read while the products of the one before run.  The barrier of a stage stands behind the first
+        // products of its last K step: by then every fragment of it is in registers, so the slot is free for the stage NS further on, and
+        // the next stage, requested NS - 1 stages ago, has landed.
         for (int s = s0; s < s1; ++s) {
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            wait_vmcnt<(NS - 2) * (UA + UB)>();            // this wavefront's share of the stage has landed
-            __builtin_amdgcn_s_barrier();                  // everyone's; and everyone has read the slot that is requested next
-            asm volatile("" ::: "memory");
-            request(s + NS - 1, slot == 0 ? NS - 1 : slot - 1);
-            const unsigned char *sa = smem + slot * Sh::STAGE, *sb = sa + Sh::MT * 128;
+            const int next = slot + 1 == NS ? 0 : slot + 1;
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
-                bf16x8 fa[FM], fb[FN];
+                constexpr int I = FM * FN, R = FM + FN, K0 = I > 2 ? 1 : 0;
+                const int cur = kk & 1;
+                const bool last = kk == 3;
 #pragma unroll
-                for (int i = 0; i < FM; ++i) fa[i] = fragment<AK, Sh::MT>(sa, la, ma + 32 * i, kk);
+                for (int i = 0; i < I; ++i) {
+                    pin();
+                    acc[i % FM][i / FM] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[cur][i % FM], fb[cur][i / FM], acc[i % FM][i / FM], 0, 0, 0);
+                    pin();
+                    if (last && i == K0) {
+                        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                        wait_vmcnt<(NS - 2) * U>();
+                        __builtin_amdgcn_s_barrier();
+                        asm volatile("" ::: "memory");
+                        pin();
+                    }
+                    const int first = last ? K0 : 0;       // reads and copies are spread over the products from here on
 #pragma unroll
-                for (int j = 0; j < FN; ++j) fb[j] = fragment<BK, Sh::NT>(sb, lb, nb + 32 * j, kk);
+                    for (int f = 0; f < R; ++f)
+                        if (f * (I - first) / R + first == i) read(cur ^ 1, f, last ? next : slot, (kk + 1) & 3);
+                    if (last)
 #pragma unroll
-                for (int i = 0; i < FM; ++i)
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+                        for (int u = 0; u < U; ++u)
+                            if (u * (I - first) / U + first == i) request(u, s + NS, slot);
+                }
             }
-            slot = slot + 1 == NS ? 0 : slot + 1;
+            slot = next;
         }
         wait_vmcnt<0>();                                   // no copy is under way when the workgroup gives its LDS back
     }
