@@ -140,8 +140,12 @@ loss_rows_kernel(const uint16_t *X, int64_t ldX, int32_t D, const int32_t *from,
     }
 }
 
+constexpr float kLog2e = 1.4426950408889634f;
+__device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
 // ---- what the tiles of logits end with: rows m are vocabulary entries, columns n tokens
-template <bool STORE> struct LossStats {
+// STORE: the logits too, for a delta kernel; SUM: the exponentials (else that kernel forms them)
+template <bool STORE, bool SUM> struct LossStats {
     struct Args { const int32_t *target; float *hit; float2 *part; int64_t Tp, first; int32_t V; float *logits; int64_t ld; };
     template <int FM, int FN>
     static __device__ inline void run(const Args &a, f32x16 (&acc)[FM][FN], int64_t m, int64_t n, int, int64_t live) {
@@ -153,16 +157,21 @@ template <bool STORE> struct LossStats {
         for (int j = 0; j < FN; ++j) {
             const int64_t t = n + 32 * j + l32;
             const int y = t < live ? a.target[t] - v0 : -1;
-            float hit = 0.0f;
+            const bool here = y >= 0 && y < 32 * FM && (y & 4) == 0;
+            if (__any(here)) {
+                float hit = 0.0f;
 #pragma unroll
-            for (int i = 0; i < FM; ++i)
+                for (int i = 0; i < FM; ++i)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    const int at = 32 * i + 8 * (v >> 2) + (v & 3);
-                    hit = y == at ? acc[i][j][v] : hit;
-                    acc[i][j][v] = at < over ? acc[i][j][v] : -INFINITY;
-                }
-            if (y >= 0 && y < 32 * FM && (y & 4) == 0) a.hit[t] = hit;
+                    for (int v = 0; v < 16; ++v) hit = y == 32 * i + 8 * (v >> 2) + (v & 3) ? acc[i][j][v] : hit;
+                if (here) a.hit[t] = hit;
+            }
+            if (over < 32 * FM) {                           // the end of the vocabulary
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) acc[i][j][v] = 32 * i + 8 * (v >> 2) + (v & 3) < over ? acc[i][j][v] : -INFINITY;
+            }
             if (STORE && t < live) {
 #pragma unroll
                 for (int i = 0; i < FM; ++i)
@@ -180,13 +189,15 @@ template <bool STORE> struct LossStats {
 #pragma unroll
                 for (int v = 0; v < 16; ++v) top = fmaxf(top, acc[i][j][v]);
             top = fmaxf(top, __shfl_xor(top, 32, 64));
-            const float ref = top == -INFINITY ? 0.0f : top;
             float sum = 0.0f;
+            if (SUM) {
+                const float ref = (top == -INFINITY ? 0.0f : top) * kLog2e;
 #pragma unroll
-            for (int i = 0; i < FM; ++i)
+                for (int i = 0; i < FM; ++i)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) sum += __expf(acc[i][j][v] - ref);
-            sum += __shfl_xor(sum, 32, 64);
+                    for (int v = 0; v < 16; ++v) sum += exp2_of(__builtin_fmaf(acc[i][j][v], kLog2e, -ref));
+                sum += __shfl_xor(sum, 32, 64);
+            }
             if (half == 0 && t < live) a.part[part * a.Tp + t] = make_float2(top, sum);
         }
     }
@@ -352,7 +363,7 @@ loss_join_kernel(LossTokens w, int64_t Tp, int64_t parts, float *nll, float *lse
 
 // A token's logits of a piece become an operand of the products, without the target's entry.  Grid (tokens, shares of the row).
 //   RUN      p = exp(z - m), m the maximum so far; top, sum, shrink go on (one share)
-//   else     delta = w exp(z - lse), with its loss (the piece is the vocabulary)
+//   else     delta = w exp(z - lse), with its loss (the piece is the vocabulary; the parts hold sums)
 //   FEW      in two terms, rows t and t + kFew
 // Rows behind the live tokens, up to a whole stage, are zeros.
 template <bool RUN, bool FEW>
@@ -380,6 +391,44 @@ loss_delta_kernel(LossTokens w, int64_t Tp, int64_t parts, int64_t first, int64_
         for (int64_t c = c0 + 4 * tid; c < c1; c += 1024) put(c, zero);
         return;
     }
+    const int64_t y = w.target[t] - first;
+    const float *z = w.logits + t * ld;
+    float ref, scale = 1.0f;
+    if (RUN) {
+        const float before = first ? w.top[t] : -INFINITY, sum_before = first ? w.sum[t] : 0.0f;
+        float top = before;
+        for (int64_t p = tid; p < parts; p += 256) top = fmaxf(top, w.part[p * Tp + t].x);
+#pragma unroll
+        for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
+        if ((tid & 63) == 0) s_top[tid >> 6] = top;
+        __syncthreads();
+        top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+        ref = top == -INFINITY ? 0.0f : top;
+        float sum = 0.0f;
+        for (int64_t c = 4 * tid; c < width; c += 1024) {
+            const float4 v = *(const float4 *)(z + c);
+            const float f[4] = {v.x, v.y, v.z, v.w};
+            float x[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                x[u] = __expf(f[u] - ref);
+                sum += x[u];
+                if (c + u == y) x[u] = 0.0f;
+            }
+            put(c, x);
+        }
+#pragma unroll
+        for (int d = 32; d > 0; d /= 2) sum += __shfl_xor(sum, d, 64);
+        if ((tid & 63) == 0) s_sum[tid >> 6] = sum;
+        __syncthreads();
+        if (tid == 0) {
+            const float shrink = before == -INFINITY ? 0.0f : __expf(before - ref);
+            w.top[t] = top;
+            w.sum[t] = sum_before * shrink + ((s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]));
+            w.shrink[t] = shrink;
+        }
+        return;
+    }
     float top = -INFINITY, sum = 0.0f;
     for (int64_t p = tid; p < parts; p += 256) {
         const float2 x = w.part[p * Tp + t];
@@ -395,26 +444,15 @@ loss_delta_kernel(LossTokens w, int64_t Tp, int64_t parts, int64_t first, int64_
     top = s_top[0]; sum = s_sum[0];
 #pragma unroll
     for (int i = 1; i < 4; ++i) join_pair(top, sum, s_top[i], s_sum[i]);
-    float ref, scale = 1.0f;
-    if (RUN) {
-        const float before = first ? w.top[t] : -INFINITY, sum_before = first ? w.sum[t] : 0.0f;
-        __syncthreads();                                    // read before any thread writes it
-        join_pair(top, sum, before, sum_before);
-        ref = top;
-        if (tid == 0) { w.top[t] = top; w.sum[t] = sum; w.shrink[t] = __expf(before - top); }
-    } else {
-        ref = top + logf(sum);
-        scale = w.weight[t];
-        if (tid == 0 && blockIdx.y == 0) {
-            const float one = loss_of(top, sum, w.hit[t]);
-            const int64_t at = w.token[t];
-            w.pull[t] = scale * expm1f(-one);
-            nll[at] = one;
-            if (lse) lse[at] = ref;
-        }
+    ref = top + logf(sum);
+    scale = w.weight[t];
+    if (tid == 0 && blockIdx.y == 0) {
+        const float one = loss_of(top, sum, w.hit[t]);
+        const int64_t at = w.token[t];
+        w.pull[t] = scale * expm1f(-one);
+        nll[at] = one;
+        if (lse) lse[at] = ref;
     }
-    const int64_t y = w.target[t] - first;
-    const float *z = w.logits + t * ld;
     for (int64_t c = c0 + 4 * tid; c < c1; c += 1024) {
         const float4 v = *(const float4 *)(z + c);
         const float f[4] = {v.x, v.y, v.z, v.w};
@@ -537,15 +575,15 @@ static LossPlan loss_plan(int64_t T, int32_t D, int32_t V, bool want_dH, bool wa
     if (p.tile_n == 256) p.parts = p.Vp / 128;
     if (p.tile_n == 128) p.parts = p.Vp / 64;
     const bool gradient = want_dH || want_dW;
-    // A piece: logits and delta of up to 768 MB.  (Their 10 bytes a logit come from memory at any size that is worth its additions to
-    // the planes.)  With dW one piece of up to 1.5 GB saves the second pass.  Few tokens: one piece.
-    const int64_t budget = (int64_t)(want_dW ? 1536 : 768) << 20, cus = compute_units();
+    // A piece: logits and delta of up to 1.5 GB.  (Their 10 bytes a logit come from memory at any size that is worth its additions to
+    // the planes, and more tiles fill their last round better.)  With dW one piece saves the second pass.  Few tokens: one piece.
+    const int64_t budget = (int64_t)1536 << 20, cus = compute_units();
     const int64_t ntiles = (T + p.tile_n - 1) / p.tile_n;
     p.one_pass = T <= kFew || p.Tp * p.Vp * 6 <= budget;
     int64_t piece = p.Vp;
     if (!p.one_pass) {
         // whole rounds of tiles of the chip, if all tokens are live
-        int64_t m = ((int64_t)768 << 20) / (6 * p.Tp) / 256;
+        int64_t m = budget / (6 * p.Tp) / 256;
         if (m < 8) m = 8;
         const int64_t rounds = m * ntiles / cus;
         if (rounds > 0) m = rounds * cus / ntiles > 0 ? rounds * cus / ntiles : 1;
@@ -554,7 +592,7 @@ static LossPlan loss_plan(int64_t T, int32_t D, int32_t V, bool want_dH, bool wa
     }
     p.piece = piece;
     const int64_t tiles = ((D + 255) / 256) * ntiles, stages = piece / 64;
-    int64_t splits = tiles > 0 ? 2 * cus / tiles : 1;
+    int64_t splits = tiles > 0 ? cus / tiles : 1;
     if (splits > stages / 8) splits = stages / 8;
     if (splits < 1) splits = 1;
     p.splits = (int32_t)splits;
@@ -662,16 +700,17 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
     const int per_part = p.tile_n == 256 ? 128 : p.tile_n == 128 ? 64 : 32;
 
     // first pass: the losses, and dH unless delta comes with dW
-    const bool run = dH && !one_pass;
+    const bool run = dH && (!one_pass || (!dW && T >= 256));    // (fewer tokens: their rows are shared out, which takes lse first)
     for (int64_t v0 = 0; T > 0 && v0 < V && rc == QLESS_OK; v0 += piece) {
         const int64_t n = rows_of(v0), np = up_to(n, 256);
         const ProductOperand rows = head(v0);
         const ProductArgs a{rows, tokens, T, p.Dp, w.count, nullptr, (int32_t)(np / 256), 1};
         if (!dH && !one_pass) {
-            rc = loss_product<LossStats<false>, ALONG, ALONG>(p.tile_n, a, LossStats<false>::Args{w.target, w.hit, w.part, p.Tp, v0, V, nullptr, 0}, st);
+            rc = loss_product<LossStats<false, true>, ALONG, ALONG>(p.tile_n, a, LossStats<false, true>::Args{w.target, w.hit, w.part, p.Tp, v0, V, nullptr, 0}, st);
             continue;
         }
-        rc = loss_product<LossStats<true>, ALONG, ALONG>(p.tile_n, a, LossStats<true>::Args{w.target, w.hit, w.part, p.Tp, v0, V, w.logits, piece}, st);
+        if (run) rc = loss_product<LossStats<true, false>, ALONG, ALONG>(p.tile_n, a, LossStats<true, false>::Args{w.target, w.hit, w.part, p.Tp, v0, V, w.logits, piece}, st);
+        else rc = loss_product<LossStats<true, true>, ALONG, ALONG>(p.tile_n, a, LossStats<true, true>::Args{w.target, w.hit, w.part, p.Tp, v0, V, w.logits, piece}, st);
         if (rc != QLESS_OK) break;
         int64_t shares = run || T >= 1024 ? 1 : 1024 / T + 1;                  // of a row
         if (shares > np / 1024) shares = np / 1024 > 0 ? np / 1024 : 1;
