@@ -313,6 +313,168 @@ checkpoint_grad_kernel(GradArgs a) {
     }
 }
 
+// The same for bfloat16 gradients and operands whose rows are whole 16-byte chunks.  A workgroup takes RT rows of R x GROUPS groups, a
+// wavefront of it one group (or half of one); stages of 32 tokens' codes, gradients and steps are copied to a ring of NS in LDS
+// without passing through registers, three of them on their way while one is used: codes stay 8 bits wide until the transposing
+// reads have brought eight tokens of a column into a lane, gradients take their step in the lane too.  Bound: memory while R is a
+// rank of adapters (codes are read once for 128 rows); the vector work of a stage, 12 operations for eight codes and 40 for eight
+// gradients, takes a third of that time at R = 16.
+// Rows of 128 codes are exchanged by 16-byte chunks, rows of gradients by 32-byte pieces, so that the eight (four) rows of each of two
+// lane groups lie in different banks.
+template <int RT> struct GradRing {
+    static constexpr int GROUPS = RT >= 128 ? 2 : 4, KT = 32, NS = 4, CM = GROUPS * 2, CN = RT / 16;
+    static constexpr int CODES = GROUPS * KT * 128, Y = KT * RT * 2, STAGE = CODES + Y + 1024, LDS = NS * STAGE;
+    static constexpr int UC = GROUPS, YQ = Y / 1024, UY = (YQ + 3) / 4, U = UC + UY + 1;
+    static_assert((NS - 2) * U < 64, "vmcnt is a 6-bit counter");
+};
+__device__ inline void global_to_lds4(const void *base, unsigned lane_off, unsigned lds_addr) {      // lane L: LDS bytes [lds_addr + 4 L, + 4)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" :: "s"(lds_addr), "v"(lane_off), "s"(base) : "memory");
+}
+
+template <int RT, class Out>
+__global__ void __launch_bounds__(256, 2)
+checkpoint_grad_ring_kernel(GradArgs a) {
+    typedef GradRing<RT> Sh;
+    constexpr int GROUPS = Sh::GROUPS, KT = Sh::KT, NS = Sh::NS, CM = Sh::CM, CN = Sh::CN, YL = RT / 8;      // YL: lanes of a row of gradients
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int64_t tiles = (int64_t)a.rtiles * a.dtiles, j = blockIdx.x / tiles;
+    const int tile = (int)(blockIdx.x - j * tiles), rt = tile / a.dtiles, gt = (tile - rt * a.dtiles) * GROUPS;
+    Segment seg;
+    if (!find_segment(a, j, seg)) return;                  // the whole workgroup
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, quad = lane >> 4;
+    const unsigned lds0 = (unsigned)(uintptr_t)((__attribute__((address_space(3))) unsigned char *)smem);
+    const int groups = (a.D + kGroup - 1) / kGroup, r0 = rt * RT;
+    const int gl = RT >= 128 ? wave >> 1 : wave, c0 = RT >= 128 ? (wave & 1) * 64 : 0, g = gt + gl < groups ? gt + gl : groups - 1;
+    auto yswizzle = [](int k) { return RT >= 128 ? k & 7 : RT == 64 ? (k >> 1) & 3 : RT == 32 ? (k >> 2) & 1 : 0; };
+    auto swizzle = [](int k) { return ((k >> 1) & 3) | ((k >> 4) & 1) << 2; };
+
+    // ---- copies: what lane and wavefront take of a stage; rows past the segment repeat its last one, bytes past a row's end its last chunk
+    const int len = (int)(seg.hi - seg.lo), stages = (len + KT - 1) / KT;
+    unsigned ccol[Sh::UC], ycol[Sh::UY];
+    int crow[Sh::UC], yrow[Sh::UY];
+#pragma unroll
+    for (int u = 0; u < Sh::UC; ++u) {
+        const int q = wave * Sh::UC + u;
+        crow[u] = 8 * (q & 3) + (lane >> 3);
+        const int at = (gt + (q >> 2)) * kGroup + ((lane & 7) ^ swizzle(crow[u])) * 16;
+        ccol[u] = (unsigned)(at < a.D - 16 ? at : a.D - 16);
+    }
+#pragma unroll
+    for (int u = 0; u < Sh::UY; ++u) {
+        const int q = wave * Sh::UY + u < Sh::YQ ? wave * Sh::UY + u : Sh::YQ - 1;
+        yrow[u] = q * (64 / YL) + lane / YL;
+        const int at = r0 * 2 + ((lane % YL) ^ (yswizzle(yrow[u]) << 1)) * 16;
+        ycol[u] = (unsigned)(at < a.R * 2 - 16 ? at : a.R * 2 - 16);
+    }
+    const unsigned ldC = (unsigned)a.ldC, ldY = (unsigned)a.ldY * 2, ldS = (unsigned)a.ldS * 4;
+    auto request = [&](int s, int slot) {
+        if (s > stages - 1) s = stages - 1;                // repeated past the end: all stages count alike
+        const int64_t t = seg.lo + (int64_t)s * KT;
+        const int last = len - s * KT - 1;                 // row
+        const unsigned at = lds0 + (unsigned)(slot * Sh::STAGE);
+        const unsigned char *c = (const unsigned char *)a.codes + t * a.ldC, *y = (const unsigned char *)a.dY + t * a.ldY * 2;
+#pragma unroll
+        for (int u = 0; u < Sh::UC; ++u) global_to_lds16(c, (unsigned)(crow[u] < last ? crow[u] : last) * ldC + ccol[u], at + (unsigned)((wave * Sh::UC + u) * 1024));
+#pragma unroll
+        for (int u = 0; u < Sh::UY; ++u) {
+            const int q = wave * Sh::UY + u < Sh::YQ ? wave * Sh::UY + u : Sh::YQ - 1;
+            global_to_lds16(y, (unsigned)(yrow[u] < last ? yrow[u] : last) * ldY + ycol[u], at + (unsigned)(Sh::CODES + q * 1024));
+        }
+        const int row = lane & 31;
+        global_to_lds4(a.step + t * a.ldS + g, (unsigned)(row < last ? row : last) * ldS, at + (unsigned)(Sh::CODES + Sh::Y + wave * 256));
+    };
+
+    // ---- operands: a lane's eight tokens are 4 quad .. + 3 and 16 + 4 quad .. + 3
+    const int krow = (l16 >> 1) < 4 ? 4 * quad + (l16 >> 1) : 12 + 4 * quad + (l16 >> 1);
+    const unsigned c_lane = (unsigned)(gl * KT * 128 + krow * 128 + (((swizzle(krow) ^ (c0 >> 4)) << 4) | (l16 & 1) << 3));
+    const int yk = 4 * quad + (l16 >> 2);
+    const unsigned y_lane = (unsigned)(Sh::CODES + yk * RT * 2 + (yswizzle(yk) << 5) + (l16 & 3) * 8);
+    const unsigned s_lane = (unsigned)(Sh::CODES + Sh::Y + wave * 256 + quad * 16);
+    typedef __attribute__((address_space(3))) i16x4 lds16x4;
+    typedef __attribute__((ext_vector_type(2))) int i32x2;
+    typedef __attribute__((address_space(3))) i32x2 lds32x2;
+
+    f32x4 acc[CM][CN];
+#pragma unroll
+    for (int m = 0; m < CM; ++m)
+#pragma unroll
+        for (int n = 0; n < CN; ++n) acc[m][n] = f32x4{0, 0, 0, 0};
+    if (stages > 0) {
+#pragma unroll
+        for (int i = 0; i < NS - 1; ++i) request(i, i);
+        int slot = 0;
+        for (int s = 0; s < stages; ++s) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            wait_vmcnt<(NS - 2) * Sh::U>();                // this wavefront's share of the stage has landed
+            __builtin_amdgcn_s_barrier();                  // everyone's; and everyone has read the slot that is requested next
+            asm volatile("" ::: "memory");
+            request(s + NS - 1, slot == 0 ? NS - 1 : slot - 1);
+            const unsigned char *st = smem + slot * Sh::STAGE;
+            float w[8];
+            const f32x4 w0 = *(const f32x4 *)(st + s_lane), w1 = *(const f32x4 *)(st + s_lane + 64);
+            const int left = len - s * KT;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { w[i] = w0[i]; w[4 + i] = w1[i]; }
+            if (left < KT) {                               // the last stage: tokens past the segment weigh nothing
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    w[i] = 4 * quad + i < left ? w[i] : 0.0f;
+                    w[4 + i] = 16 + 4 * quad + i < left ? w[4 + i] : 0.0f;
+                }
+            }
+            bf16x8 fy[2][CN];                              // gradient times step in two terms
+#pragma unroll
+            for (int n = 0; n < CN; ++n) {
+                const unsigned char *p = st + (y_lane ^ (unsigned)(n << 5));
+                const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)p);
+                const i16x4 z = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)(p + 16 * RT * 2));
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float v = __fmul_rn(bf16_value((uint16_t)(i < 4 ? x[i & 3] : z[i & 3])), w[i]);
+                    fy[0][n][i] = (__bf16)v;
+                    fy[1][n][i] = (__bf16)__fsub_rn(v, (float)fy[0][n][i]);
+                }
+            }
+#pragma unroll
+            for (int m = 0; m < CM; ++m) {
+                const i32x2 b = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds32x2 *)(st + (c_lane ^ (unsigned)(m << 4))));
+                union { uint32_t u[4]; bf16x8 v; } fc;
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    const int x = b[h >> 1] >> (16 * (h & 1));
+                    fc.u[h] = __builtin_amdgcn_perm(__float_as_uint((float)(int8_t)(x >> 8)), __float_as_uint((float)(int8_t)x), 0x07060302u);
+                }
+#pragma unroll
+                for (int term = 1; term >= 0; --term)
+#pragma unroll
+                    for (int n = 0; n < CN; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fc.v, fy[term][n], acc[m][n], 0, 0, 0);
+            }
+            slot = slot + 1 == NS ? 0 : slot + 1;
+        }
+        wait_vmcnt<0>();                                   // no copy is under way when the workgroup gives its LDS back
+    }
+    // a lane holds four columns of one row (D is a multiple of four)
+    if (gt + gl >= groups) return;
+#pragma unroll
+    for (int n = 0; n < CN; ++n) {
+        const int r = r0 + n * 16 + l16;
+        if (r >= a.R) continue;
+#pragma unroll
+        for (int m = 0; m < CM; ++m) {
+            const int d = g * kGroup + c0 + m * 16 + quad * 4;
+            if (d >= a.D) continue;
+            if (!seg.whole) {
+                *(f32x4 *)(a.planes + (j * a.R + r) * (int64_t)a.D + d) = acc[m][n];
+            } else {
+                Out x[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = sizeof(Out) == 2 ? (Out)bf16_bits(acc[m][n][i]) : (Out)acc[m][n][i];
+                __builtin_memcpy((Out *)a.G + seg.e * a.ldG + (int64_t)r * a.D + d, x, sizeof x);
+            }
+        }
+    }
+}
+
 // The planes of the examples of more than one segment, added in the order of their tokens.
 template <class Out>
 __global__ void __launch_bounds__(256)
@@ -343,6 +505,13 @@ static int64_t grad_chunk(int64_t T, int64_t n, int32_t R, int32_t D) {
 }
 static int64_t grad_segments(int64_t T, int64_t n, int64_t chunk) { return n + T / chunk; }
 
+template <class Out>
+static void launch_join(const GradArgs &a, hipStream_t st) {
+    if (a.segments <= a.n) return;
+    int64_t bx = ((int64_t)a.R * a.D + 1023) / 1024;
+    if (bx > 1024) bx = 1024;
+    hipLaunchKernelGGL(checkpoint_join_kernel<Out>, dim3((unsigned)bx, (unsigned)a.n), dim3(256), 0, st, a);
+}
 template <int RT, class Y, int TERMS, class Out>
 static qless_status launch_grad(GradArgs a, hipStream_t st) {
     a.rtiles = (a.R + RT - 1) / RT;
@@ -350,12 +519,26 @@ static qless_status launch_grad(GradArgs a, hipStream_t st) {
     const int64_t grid = a.segments * a.rtiles * a.dtiles;
     if (grid > 0x7FFFFFFF) return QLESS_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((checkpoint_grad_kernel<RT, Y, TERMS, Out>), dim3((unsigned)grid), dim3(256), 0, st, a);
-    if (a.segments > a.n) {
-        int64_t bx = ((int64_t)a.R * a.D + 1023) / 1024;
-        if (bx > 1024) bx = 1024;
-        hipLaunchKernelGGL(checkpoint_join_kernel<Out>, dim3((unsigned)bx, (unsigned)a.n), dim3(256), 0, st, a);
-    }
+    launch_join<Out>(a, st);
     return launch_status();
+}
+template <int RT, class Out>
+static qless_status launch_ring(GradArgs a, hipStream_t st) {
+    QLESS_LDS_KERNEL((checkpoint_grad_ring_kernel<RT, Out>), GradRing<RT>::LDS);
+    a.rtiles = (a.R + RT - 1) / RT;
+    a.dtiles = (a.D + kGroup * GradRing<RT>::GROUPS - 1) / (kGroup * GradRing<RT>::GROUPS);
+    const int64_t grid = a.segments * a.rtiles * a.dtiles;
+    if (grid > 0x7FFFFFFF) return QLESS_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((checkpoint_grad_ring_kernel<RT, Out>), dim3((unsigned)grid), dim3(256), GradRing<RT>::LDS, st, a);
+    launch_join<Out>(a, st);
+    return launch_status();
+}
+template <class Out>
+static qless_status launch_ring_rows(const GradArgs &a, hipStream_t st) {
+    if (a.R <= 16) return launch_ring<16, Out>(a, st);
+    if (a.R <= 32) return launch_ring<32, Out>(a, st);
+    if (a.R <= 64) return launch_ring<64, Out>(a, st);
+    return launch_ring<128, Out>(a, st);
 }
 template <class Y, int TERMS, class Out>
 static qless_status launch_grad_rows(const GradArgs &a, hipStream_t st) {
@@ -428,8 +611,13 @@ extern "C" qless_status qless_checkpoint8_grad(const void *dY, qless_dtype dtY, 
     a.segments = grad_segments(T, n, a.chunk);
     const size_t need = qless_checkpoint8_grad_workspace(T, n, R, D);
     if (need > 0 && (!ws || ws_bytes < need || ((uintptr_t)ws & 15) != 0)) return QLESS_ERR_WORKSPACE;
+    const qless_status ready = device_ready();
+    if (ready != QLESS_OK) return ready;
     const hipStream_t st = (hipStream_t)stream;
-    if (dtY == QLESS_BF16)
-        return dtG == QLESS_BF16 ? launch_grad_rows<uint16_t, 1, uint16_t>(a, st) : launch_grad_rows<uint16_t, 2, float>(a, st);
-    return dtG == QLESS_BF16 ? launch_grad_rows<float, 1, uint16_t>(a, st) : launch_grad_rows<float, 3, float>(a, st);
+    // 16-byte copies and 32-bit offsets
+    const bool whole = dtY == QLESS_BF16 && R % 8 == 0 && D % 16 == 0 && (T <= 1 || (ldY % 8 == 0 && ldC % 16 == 0)) &&
+                       (((uintptr_t)dY | (uintptr_t)codes) & 15) == 0 && ldY < (1 << 24) && ldC < (1 << 24) && ldS < (1 << 24) && T <= 0x3FFFFFFF;
+    if (whole) return dtG == QLESS_BF16 ? launch_ring_rows<uint16_t>(a, st) : launch_ring_rows<float>(a, st);
+    if (dtY == QLESS_BF16) return dtG == QLESS_BF16 ? launch_grad_rows<uint16_t, 2, uint16_t>(a, st) : launch_grad_rows<uint16_t, 2, float>(a, st);
+    return dtG == QLESS_BF16 ? launch_grad_rows<float, 2, uint16_t>(a, st) : launch_grad_rows<float, 3, float>(a, st);
 }

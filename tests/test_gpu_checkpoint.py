@@ -3,8 +3,8 @@
 Codes, steps and what they are read back as are whole or exactly defined: they have to be equal.  A gradient is a sum of L terms.
 With fp32 results the terms are exact (bfloat16 dY) or off by 2^-24 of themselves (fp32 dY, in three bfloat16 parts), and the matrix
 cores and the joins add them in fp32, each of at most L + 64 additions off by at most one step, 2^-23 of a partial sum that is at most
-the sum S of the terms' absolute values: |error| <= (L + 64) 2^-23 S.  bfloat16 results add the rounding of dY * step, 2^-8 of
-every term, and their own, 2^-8 of the result."""
+the sum S of the terms' absolute values: |error| <= (L + 64) 2^-23 S.  bfloat16 results add the rounding of a factor to bfloat16, 2^-8
+of every term at most, and their own, 2^-8 of the result."""
 import pytest
 import torch
 
@@ -125,23 +125,39 @@ CASES = [  # R, D, ends
     (8, 256, [0, 10, 4000, 4003]),
     (300, 129, [0, 2500]),
 ]
+WHOLE = [  # R in eights, D in sixteens: rows of whole chunks
+    (8, 16, [0, 1]),
+    (16, 144, [0, 31, 32, 64, 129]),
+    (24, 528, [2, 35, 35, 200]),
+    (32, 512, [0, 100]),
+    (40, 48, [0, 0, 33, 90]),
+    (64, 1040, [0, 65, 70]),
+    (72, 256, [5, 6, 134]),
+    (128, 640, [0, 257, 300]),
+    (136, 400, [0, 96, 97]),
+    (16, 128, [0, 5000]),
+    (8, 1024, [0, 10, 4000, 4003]),
+    (256, 272, [0, 2500, 5000]),
+    (520, 1040, [0, 200, 333]),
+]
 
 
 @pytest.mark.parametrize("dtY,dtG", [(torch.bfloat16, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.float32, torch.float32),
                                      (torch.float32, torch.bfloat16)])
-@pytest.mark.parametrize("R,D,ends", CASES)
-def test_weight_gradients(R, D, ends, dtY, dtG):
-    _say("gradient R=%d D=%d ends=%s %s %s" % (R, D, ends, dtY, dtG))
+@pytest.mark.parametrize("R,D,ends,pad", [(*c, 1) for c in CASES] + [(*c, 0) for c in WHOLE])
+def test_weight_gradients(R, D, ends, pad, dtY, dtG):
+    _say("gradient R=%d D=%d ends=%s pad=%d %s %s" % (R, D, ends, pad, dtY, dtG))
     T = ends[-1] + 9                                  # tokens behind the last example
     codes, steps = plain.checkpoint(_inputs(T, D, R + D))
     g = torch.Generator().manual_seed(R * D)
     dY = (torch.randn(T, R, generator=g) * torch.exp(torch.randn(T, 1, generator=g)) * 1e-3).to(dtY)
     ref, size = plain.weight_gradients(dY, codes, steps, ends)
-    dY[:ends[0]] = float("nan")                       # neither these nor the ones behind are read
-    dY[ends[-1]:] = float("nan")
-    y, _ = _inside(dY, 1, 2)
-    q, _ = _inside(codes.to(torch.int8), 3, 1)
-    s, _ = _inside(steps.float(), 0, 1)
+    for x in (dY, steps):                             # neither these nor the ones behind are read
+        x[:ends[0]] = float("nan")
+        x[ends[-1]:] = float("nan")
+    y, _ = _inside(dY, pad, 2 * pad)
+    q, _ = _inside(codes.to(torch.int8), 3 * pad, pad)
+    s, _ = _inside(steps.float(), 0, pad)
     off = torch.tensor(ends, device=DEV)
     G = Q.checkpoint8_grad(y, q, s, off, dtype=dtG)
     assert G.shape == ref.shape and G.dtype == dtG
