@@ -6,15 +6,12 @@
 // to even, so that |code| <= 127.  Eight bits of step cost at most 1/128 of resolution, and buy products: a code (7 bits) is a
 // bfloat16, and a bfloat16 gradient times a step (16 bits) is the sum of two, so that the backward pass is exact up to its
 // fp32 sums with two matrix products instead of three.  A group with an infinity or a NaN gets the step NaN and codes 0.
-#include "common.h"
+#include "product.h"
+#include "score.h"
 
 namespace qless {
 
-typedef __attribute__((ext_vector_type(4))) int i32x4;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(4))) short i16x4;
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
 constexpr int kGroup = QLESS_CHECKPOINT_GROUP;
 
@@ -161,17 +158,21 @@ __device__ inline int64_t offset_at(const GradArgs &a, int64_t e) {      // neve
     const int64_t o = a.offsets[e];
     return o < 0 ? 0 : (o > a.T ? a.T : o);
 }
-__device__ inline int64_t phi(const GradArgs &a, int64_t e) { return e + offset_at(a, e) / a.chunk; }
-__device__ inline bool find_segment(const GradArgs &a, int64_t j, Segment &s) {
-    if (j < phi(a, 0) || j >= phi(a, a.n)) return false;
-    int64_t lo = 0, hi = a.n;                              // phi(lo) <= j < phi(hi)
+__device__ inline int64_t phi(const GradArgs &a, int64_t e, int64_t chunk) { return e + offset_at(a, e) / chunk; }
+__device__ inline int64_t find_example(const GradArgs &a, int64_t j, int64_t chunk) {     // phi(example) <= j < phi(example + 1), or -1
+    if (j < phi(a, 0, chunk) || j >= phi(a, a.n, chunk)) return -1;
+    int64_t lo = 0, hi = a.n;
     while (hi - lo > 1) {
         const int64_t mid = (lo + hi) >> 1;
-        if (phi(a, mid) <= j) lo = mid; else hi = mid;
+        if (phi(a, mid, chunk) <= j) lo = mid; else hi = mid;
     }
-    const int64_t o0 = offset_at(a, lo), o1 = offset_at(a, lo + 1), i = j - (lo + o0 / a.chunk);
+    return lo;
+}
+__device__ inline bool find_segment(const GradArgs &a, int64_t j, Segment &s) {
+    s.e = find_example(a, j, a.chunk);
+    if (s.e < 0) return false;
+    const int64_t o0 = offset_at(a, s.e), o1 = offset_at(a, s.e + 1), i = j - (s.e + o0 / a.chunk);
     const int64_t c0 = (o0 / a.chunk + i) * a.chunk, c1 = c0 + a.chunk;
-    s.e = lo;
     s.lo = c0 > o0 ? c0 : o0;
     s.hi = c1 < o1 ? c1 : o1;
     s.whole = o0 / a.chunk == o1 / a.chunk;
@@ -479,8 +480,8 @@ checkpoint_grad_ring_kernel(GradArgs a) {
 template <class Out>
 __global__ void __launch_bounds__(256)
 checkpoint_join_kernel(GradArgs a) {
-    const int64_t e = blockIdx.y, size = (int64_t)a.R * a.D, p0 = phi(a, e);
-    int64_t p1 = phi(a, e + 1);
+    const int64_t e = blockIdx.y, size = (int64_t)a.R * a.D, p0 = phi(a, e, a.chunk);
+    int64_t p1 = phi(a, e + 1, a.chunk);
     if (p1 > a.segments) p1 = a.segments;
     if (p1 - p0 < 2) return;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
@@ -491,15 +492,92 @@ checkpoint_join_kernel(GradArgs a) {
     }
 }
 
-// Tokens of a segment: enough segments to give every compute unit a few workgroups, but none so short that its plane (written and read,
-// 8 R bytes per column) costs more than its codes.
-static int64_t grad_chunk(int64_t T, int64_t n, int32_t R, int32_t D) {
-    const int64_t rtile = R > 64 ? 128 : R > 32 ? 64 : R > 16 ? 32 : 16;
-    const int64_t tiles = ((R + rtile - 1) / rtile) * ((D + kGroup - 1) / kGroup);
-    int64_t chunk = T * tiles / 1024;
+// ---- Many rows of R (a layer's own weights): the products are the bound, so that the activations are formed once, as bfloat16 rows of
+// tokens, and the tiles of product.h multiply them with the gradients.  fp32 results take the activations as the sum of two bfloat16
+// numbers (exact: a code times its step has 15 bits), bfloat16 ones rounded once, which is half the products.
+// A workgroup 64 tokens of an example (the last ones of it with zeros behind them): block e + offset[e] / 64 and on, TERMS times 64 rows each.
+template <int TERMS>
+__global__ void __launch_bounds__(256)
+checkpoint_expand_kernel(GradArgs a, uint16_t *out, int64_t ld) {
+    const int64_t j = blockIdx.x, e = find_example(a, j, 64);
+    if (e < 0) return;
+    const int64_t o1 = offset_at(a, e + 1), t0 = offset_at(a, e) + 64 * (j - phi(a, e, 64));
+    out += j * TERMS * 64 * ld;
+    for (int64_t i = threadIdx.x; i < 64 * (ld / 8); i += 256) {
+        const int64_t r = i / (ld / 8), c = (i - r * (ld / 8)) * 8, t = t0 + r, left = t < o1 ? a.D - c : 0;
+        const int8_t *in = a.codes + t * a.ldC + c;
+        int8_t q[8];
+        if (left >= 8) __builtin_memcpy(q, in, 8);
+        else
+#pragma unroll
+            for (int u = 0; u < 8; ++u) q[u] = u < left ? in[u] : (int8_t)0;
+        const float s = left > 0 ? a.step[t * a.ldS + c / kGroup] : 0.0f;
+        float x[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) x[u] = __fmul_rn((float)q[u], s);
+#pragma unroll
+        for (int term = 0; term < TERMS; ++term) {
+            Eight<uint16_t>::store(out + (term * 64 + r) * ld + c, 8, x);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = __fsub_rn(x[u], bf16_value(bf16_bits(x[u])));
+        }
+    }
+}
+// rows m are columns of G, columns n its rows, the part of K its example
+template <class Out> struct GradStore {
+    struct Args { Out *G; int64_t ldG; int32_t R, D; };
+    template <int FM, int FN>
+    static __device__ inline void run(const Args &a, f32x16 (&acc)[FM][FN], int64_t m, int64_t n, int e, int64_t) {
+        const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const int64_t r = n + 32 * j + l32;
+            if (r >= a.R) continue;
+            Out *row = a.G + e * a.ldG + r * a.D;
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int64_t d = m + 32 * i + 8 * q + 4 * half;
+                    Out x[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) x[u] = sizeof(Out) == 2 ? (Out)bf16_bits(acc[i][j][4 * q + u]) : (Out)acc[i][j][4 * q + u];
+                    if (d + 4 <= a.D) __builtin_memcpy(row + d, x, sizeof x);
+                    else
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) if (d + u < a.D) row[d + u] = x[u];
+                }
+        }
+    }
+};
+typedef ProductShape<256, 256, 2, 4, 2> GradTile;
+
+static int64_t expand_ld(int32_t D) { return ((int64_t)D + 7) / 8 * 8; }
+// Rows of R and examples that fill the chip with tiles, of tokens enough that padding them to 64 costs little.
+static bool many_rows(int64_t T, int64_t n, int32_t R, int32_t D) {
+    return R >= 256 && T >= 128 * n && n * ((R + 255) / 256) * ((D + 255) / 256) >= compute_units() / 2;
+}
+static size_t expand_bytes(int64_t T, int64_t n, int32_t D, int terms) { return (size_t)(n + T / 64) * 64 * terms * (size_t)expand_ld(D) * 2; }
+
+template <int TERMS, class Out>
+static qless_status launch_many(const GradArgs &a, hipStream_t st) {
+    uint16_t *x = (uint16_t *)a.planes;
+    const int64_t ld = expand_ld(a.D), blocks = a.n + a.T / 64;
+    if (blocks > 0x7FFFFFFF / (64 * TERMS)) return QLESS_ERR_UNSUPPORTED;
+    const ProductArgs p{ProductOperand{x, ld * 2, ld * 2, blocks * 64 * TERMS}, ProductOperand{a.dY, a.ldY * 2, (int64_t)a.R * 2, 0},
+                        a.R, a.T, nullptr, nullptr, (a.D + 255) / 256, (int32_t)a.n, a.offsets};
+    hipLaunchKernelGGL(checkpoint_expand_kernel<TERMS>, dim3((unsigned)blocks), dim3(256), 0, st, a, x, ld);
+    const qless_status rc = launch_product<GradTile, ACROSS, ACROSS, GradStore<Out>, TERMS>(p, typename GradStore<Out>::Args{(Out *)a.G, a.ldG, a.R, a.D}, st);
+    return rc == QLESS_OK ? launch_status() : rc;
+}
+
+// Tokens of a segment: two segments for each of the two workgroups of a compute unit, if all were full (the longest example would keep
+// few of them busy for long), but none so short that its plane (written and read, 8 R bytes per column) costs more than its codes.
+static int64_t grad_chunk(int64_t T, int32_t R, int32_t D) {
+    const int64_t tiles = ((R + 127) / 128) * ((D + 4 * kGroup - 1) / (4 * kGroup)) * (R > 64 ? 2 : 1);
+    int64_t chunk = T * tiles / (4 * (int64_t)compute_units());
     if (chunk < 8 * (int64_t)R) chunk = 8 * (int64_t)R;
     if (chunk < 128) chunk = 128;
-    if (n * tiles >= 512 && chunk < 4 * (T / n)) chunk = 4 * (T / n);      // enough workgroups: only an example far longer than the others is cut
     if (chunk >= T) chunk = T + 1;
     return (chunk + 63) / 64 * 64;
 }
@@ -593,8 +671,9 @@ extern "C" qless_status qless_checkpoint8_read(const int8_t *codes, int64_t ldC,
 extern "C" size_t qless_checkpoint8_grad_workspace(int64_t T, int64_t n, int32_t R, int32_t D) {
     using namespace qless;
     if (T < 0 || n < 1 || R < 1 || D < 1) return 0;
-    const int64_t segments = grad_segments(T, n, grad_chunk(T, n, R, D));
-    return segments > n ? (size_t)segments * (size_t)R * (size_t)D * 4 : 0;
+    const int64_t segments = grad_segments(T, n, grad_chunk(T, R, D));
+    const size_t planes = segments > n ? (size_t)segments * (size_t)R * (size_t)D * 4 : 0, rows = many_rows(T, n, R, D) ? expand_bytes(T, n, D, 2) : 0;
+    return planes > rows ? planes : rows;
 }
 
 extern "C" qless_status qless_checkpoint8_grad(const void *dY, qless_dtype dtY, int64_t ldY, int32_t R, const int8_t *codes, int64_t ldC,
@@ -607,7 +686,7 @@ extern "C" qless_status qless_checkpoint8_grad(const void *dY, qless_dtype dtY, 
     if (n > 1 && ldG < (int64_t)R * D) return QLESS_ERR_INVALID_ARG;
     if (n == 0) return QLESS_OK;
     if (!offsets || !G || (T > 0 && (!dY || !codes || !step))) return QLESS_ERR_INVALID_ARG;
-    GradArgs a{dY, ldY, codes, ldC, step, ldS, offsets, n, T, grad_chunk(T, n, R, D), 0, R, D, 0, 0, G, ldG, (float *)ws};
+    GradArgs a{dY, ldY, codes, ldC, step, ldS, offsets, n, T, grad_chunk(T, R, D), 0, R, D, 0, 0, G, ldG, (float *)ws};
     a.segments = grad_segments(T, n, a.chunk);
     const size_t need = qless_checkpoint8_grad_workspace(T, n, R, D);
     if (need > 0 && (!ws || ws_bytes < need || ((uintptr_t)ws & 15) != 0)) return QLESS_ERR_WORKSPACE;
@@ -615,8 +694,10 @@ extern "C" qless_status qless_checkpoint8_grad(const void *dY, qless_dtype dtY, 
     if (ready != QLESS_OK) return ready;
     const hipStream_t st = (hipStream_t)stream;
     // 16-byte copies and 32-bit offsets
-    const bool whole = dtY == QLESS_BF16 && R % 8 == 0 && D % 16 == 0 && (T <= 1 || (ldY % 8 == 0 && ldC % 16 == 0)) &&
-                       (((uintptr_t)dY | (uintptr_t)codes) & 15) == 0 && ldY < (1 << 24) && ldC < (1 << 24) && ldS < (1 << 24) && T <= 0x3FFFFFFF;
+    const bool whole_y = dtY == QLESS_BF16 && R % 8 == 0 && (T <= 1 || ldY % 8 == 0) && ((uintptr_t)dY & 15) == 0 && ldY < (1 << 22) && T <= 0x3FFFFFFF;
+    const bool whole = whole_y && D % 16 == 0 && (T <= 1 || ldC % 16 == 0) && ((uintptr_t)codes & 15) == 0 && ldC < (1 << 24) && ldS < (1 << 24);
+    if (whole_y && T > 1 && expand_ld(D) < (1 << 22) && many_rows(T, n, R, D))
+        return dtG == QLESS_BF16 ? launch_many<1, uint16_t>(a, st) : launch_many<2, float>(a, st);
     if (whole) return dtG == QLESS_BF16 ? launch_ring_rows<uint16_t>(a, st) : launch_ring_rows<float>(a, st);
     if (dtY == QLESS_BF16) return dtG == QLESS_BF16 ? launch_grad_rows<uint16_t, 2, uint16_t>(a, st) : launch_grad_rows<uint16_t, 2, float>(a, st);
     return dtG == QLESS_BF16 ? launch_grad_rows<float, 2, uint16_t>(a, st) : launch_grad_rows<float, 3, float>(a, st);

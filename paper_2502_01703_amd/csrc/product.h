@@ -30,6 +30,9 @@ struct ProductArgs {
     int64_t k;                 // steps of K
     const int32_t *live_n, *live_k;   // device: fewer of them, or null (k rounded up to a stage: the operands are zero there)
     int32_t mtiles, splits;    // splits: K in as many parts of whole stages
+    // CUTS: part e of K is the rows [cuts[e], cuts[e + 1]) of b (device; clamped to 0 .. k), its stages in a begin at stage
+    // TERMS (e + cuts[e] / 64): each 64 rows of b meet TERMS stages of a, one after another, which are zeros behind the part's rows.
+    const int64_t *cuts;
 };
 
 template <int KIND, int EXT, int NW> struct ProductCopies {
@@ -107,9 +110,10 @@ template <int MT_, int NT_, int WY_, int WX_, int NS_> struct ProductShape {
 };
 
 // Epilogue::run(args, acc, m, n, split, live): acc[i][j][v] is C at m + 32 i + 8 (v / 4) + 4 half + v % 4, n + 32 j + lane % 32.
-template <class Sh, int AK, int BK, class Epilogue>
+template <class Sh, int AK, int BK, class Epilogue, int CUTS = 0>
 __global__ void __launch_bounds__(64 * Sh::NW, Sh::NW / 4)
 product_kernel(ProductArgs p, typename Epilogue::Args e) {
+    constexpr int TERMS = CUTS ? CUTS : 1;
     constexpr int FM = Sh::FM, FN = Sh::FN, NS = Sh::NS, NW = Sh::NW;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     // Tiles in an order in which the workgroups of an XCD (ids eight apart) share operands: bands of eight column tiles, row tile by row
@@ -123,7 +127,18 @@ product_kernel(ProductArgs p, typename Epilogue::Args e) {
     const int64_t in = idx - split * plane, band = in / (8 * p.mtiles), wide = ntiles - band * 8 < 8 ? ntiles - band * 8 : 8, r = in - band * 8 * p.mtiles;
     const int m0 = __builtin_amdgcn_readfirstlane((int)(r / wide * Sh::MT)), n0 = __builtin_amdgcn_readfirstlane((int)((band * 8 + r % wide) * Sh::NT));
     const int64_t stages = (k + 63) / 64;
-    const int s0 = __builtin_amdgcn_readfirstlane((int)(stages * split / p.splits)), s1 = __builtin_amdgcn_readfirstlane((int)(stages * (split + 1) / p.splits));
+    int s0 = __builtin_amdgcn_readfirstlane((int)(stages * split / p.splits)), s1 = __builtin_amdgcn_readfirstlane((int)(stages * (split + 1) / p.splits));
+    if (CUTS) {
+        static_assert(!CUTS || BK == ACROSS, "rows of K");
+        int64_t lo = p.cuts[split], hi = p.cuts[split + 1];
+        lo = lo < 0 ? 0 : (lo > k ? k : lo);
+        hi = hi < lo ? lo : (hi > k ? k : hi);
+        const int64_t block = split + lo / 64;
+        s0 = __builtin_amdgcn_readfirstlane((int)block * TERMS);
+        s1 = s0 + __builtin_amdgcn_readfirstlane((int)((hi - lo + 63) / 64) * TERMS);
+        p.b.base = (const unsigned char *)p.b.base + (lo - 64 * block) * p.b.ld;      // stage s0 begins at row lo
+        p.b.depth = 64 * block + hi - lo;
+    }
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wy = wave / Sh::WX, wx = wave % Sh::WX;
     const unsigned lds0 = (unsigned)(uintptr_t)((__attribute__((address_space(3))) unsigned char *)smem);
@@ -137,7 +152,7 @@ product_kernel(ProductArgs p, typename Epilogue::Args e) {
         if (s > s1 - 1) s = s1 - 1;
         const unsigned at = lds0 + (unsigned)(slot * Sh::STAGE);
         if (u < UA) ca.issue(u, s, lane, wave, at);
-        else cb.issue(u - UA, s, lane, wave, at + Sh::MT * 128);
+        else cb.issue(u - UA, s / TERMS, lane, wave, at + Sh::MT * 128);
     };
     f32x16 acc[FM][FN];
 #pragma unroll
@@ -205,13 +220,13 @@ product_kernel(ProductArgs p, typename Epilogue::Args e) {
     Epilogue::template run<FM, FN>(e, acc, m0 + ma, n0 + nb, split, n);
 }
 
-template <class Sh, int AK, int BK, class Epilogue>
+template <class Sh, int AK, int BK, class Epilogue, int CUTS = 0>
 static qless_status launch_product(const ProductArgs &p, const typename Epilogue::Args &e, hipStream_t st) {
-    QLESS_LDS_KERNEL((product_kernel<Sh, AK, BK, Epilogue>), Sh::LDS);
+    QLESS_LDS_KERNEL((product_kernel<Sh, AK, BK, Epilogue, CUTS>), Sh::LDS);
     const int64_t total = p.mtiles * ((p.n + Sh::NT - 1) / Sh::NT) * p.splits, grid = (total + 7) / 8 * 8;
     if (grid > 0x7FFFFFFF) return QLESS_ERR_UNSUPPORTED;
     if (grid > 0)
-        hipLaunchKernelGGL((product_kernel<Sh, AK, BK, Epilogue>), dim3((unsigned)grid), dim3(64 * Sh::NW), Sh::LDS, st, p, e);
+        hipLaunchKernelGGL((product_kernel<Sh, AK, BK, Epilogue, CUTS>), dim3((unsigned)grid), dim3(64 * Sh::NW), Sh::LDS, st, p, e);
     return QLESS_OK;
 }
 

@@ -139,6 +139,8 @@ WHOLE = [  # R in eights, D in sixteens: rows of whole chunks
     (8, 1024, [0, 10, 4000, 4003]),
     (256, 272, [0, 2500, 5000]),
     (520, 1040, [0, 200, 333]),
+    (1032, 1995, [3, 200, 200, 455, 700]),               # tiles of expanded activations
+    (4096, 2048, [0, 300]),
 ]
 
 
