@@ -159,14 +159,23 @@ __device__ inline int64_t offset_at(const GradArgs &a, int64_t e) {      // neve
     return o < 0 ? 0 : (o > a.T ? a.T : o);
 }
 __device__ inline int64_t phi(const GradArgs &a, int64_t e, int64_t chunk) { return e + offset_at(a, e) / chunk; }
-__device__ inline int64_t find_example(const GradArgs &a, int64_t j, int64_t chunk) {     // phi(example) <= j < phi(example + 1), or -1
-    if (j < phi(a, 0, chunk) || j >= phi(a, a.n, chunk)) return -1;
-    int64_t lo = 0, hi = a.n;
-    while (hi - lo > 1) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (phi(a, mid, chunk) <= j) lo = mid; else hi = mid;
+// The example with phi(example) <= j < phi(example + 1), or -1; the whole wavefront asks, 64 examples at a time (a search by halves is a
+// chain of loads as long as a few stages of the work itself).
+__device__ inline int64_t find_example(const GradArgs &a, int64_t j, int64_t chunk) {
+    const int lane = threadIdx.x & 63;
+    int64_t lo = 0, hi = a.n;                              // phi(lo) <= j < phi(hi), once both are known
+    bool inside = j < phi(a, a.n, chunk);
+    for (;;) {
+        const int64_t step = (hi - lo + 63) / 64, e = lo + lane * step;
+        const uint64_t below = __ballot(e < hi && phi(a, e < hi ? e : lo, chunk) <= j);
+        if (below == 0) inside = false;                    // j < phi(0)
+        if (!inside) return -1;
+        const int at = 63 - __clzll((long long)below);
+        lo += at * step;
+        if (step == 1) break;
+        hi = lo + step < hi ? lo + step : hi;
     }
-    return lo;
+    return (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)lo);
 }
 __device__ inline bool find_segment(const GradArgs &a, int64_t j, Segment &s) {
     s.e = find_example(a, j, a.chunk);
@@ -317,19 +326,35 @@ checkpoint_grad_kernel(GradArgs a) {
 // The same for bfloat16 gradients and operands whose rows are whole 16-byte chunks.  A workgroup takes RT rows of R x GROUPS groups, a
 // wavefront of it one group (or half of one); stages of 32 tokens' codes, gradients and steps are copied to a ring of NS in LDS
 // without passing through registers, three of them on their way while one is used: codes stay 8 bits wide until the transposing
-// reads have brought eight tokens of a column into a lane, gradients take their step in the lane too.  Bound: memory while R is a
-// rank of adapters (codes are read once for 128 rows); the vector work of a stage, 12 operations for eight codes and 40 for eight
-// gradients, takes a third of that time at R = 16.
+// reads have brought eight tokens of a column into a lane, and the step is multiplied there, into the gradients or, from 128 rows on,
+// into the codes (either product has 16 bits: two bfloat16 numbers).  Bound: memory while R is a rank of adapters (codes are read once
+// for 128 rows); the vector work of a stage is 12 operations for eight numbers of one side and 40 for eight of the other.
 // Rows of 128 codes are exchanged by 16-byte chunks, rows of gradients by 32-byte pieces, so that the eight (four) rows of each of two
 // lane groups lie in different banks.
 template <int RT> struct GradRing {
     static constexpr int GROUPS = RT >= 128 ? 2 : 4, KT = 32, NS = 4, CM = GROUPS * 2, CN = RT / 16;
     static constexpr int CODES = GROUPS * KT * 128, Y = KT * RT * 2, STAGE = CODES + Y + 1024, LDS = NS * STAGE;
+    static constexpr bool SCALE_CODES = RT >= 128;         // the side with fewer fragments takes the steps
     static constexpr int UC = GROUPS, YQ = Y / 1024, UY = (YQ + 3) / 4, U = UC + UY + 1;
     static_assert((NS - 2) * U < 64, "vmcnt is a 6-bit counter");
 };
 __device__ inline void global_to_lds4(const void *base, unsigned lane_off, unsigned lds_addr) {      // lane L: LDS bytes [lds_addr + 4 L, + 4)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" :: "s"(lds_addr), "v"(lane_off), "s"(base) : "memory");
+}
+
+__device__ inline bf16x8 upper_halves(const float (&v)[8]) {
+    union { uint32_t u[4]; bf16x8 b; } r;
+#pragma unroll
+    for (int h = 0; h < 4; ++h) r.u[h] = __builtin_amdgcn_perm(__float_as_uint(v[2 * h + 1]), __float_as_uint(v[2 * h]), 0x07060302u);
+    return r.b;
+}
+// Numbers of at most 16 significant bits as sums of two bfloat16: their upper halves, and the rest, which has eight bits.
+__device__ inline void two_terms(const float (&v)[8], bf16x8 &first, bf16x8 &second) {
+    float rest[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rest[i] = __fsub_rn(v[i], __uint_as_float(__float_as_uint(v[i]) & 0xFFFF0000u));
+    first = upper_halves(v);
+    second = upper_halves(rest);
 }
 
 template <int RT, class Out>
@@ -423,32 +448,43 @@ checkpoint_grad_ring_kernel(GradArgs a) {
                     w[4 + i] = 16 + 4 * quad + i < left ? w[4 + i] : 0.0f;
                 }
             }
-            bf16x8 fy[2][CN];                              // gradient times step in two terms
+            bf16x8 fy[2][CN];                              // (fy[1]: the second terms, if they are the gradients')
 #pragma unroll
             for (int n = 0; n < CN; ++n) {
                 const unsigned char *p = st + (y_lane ^ (unsigned)(n << 5));
                 const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)p);
                 const i16x4 z = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)(p + 16 * RT * 2));
+                fy[0][n] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, z, 0, 1, 2, 3, 4, 5, 6, 7));
+                if (!Sh::SCALE_CODES) {
+                    float v[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float v = __fmul_rn(bf16_value((uint16_t)(i < 4 ? x[i & 3] : z[i & 3])), w[i]);
-                    fy[0][n][i] = (__bf16)v;
-                    fy[1][n][i] = (__bf16)__fsub_rn(v, (float)fy[0][n][i]);
+                    for (int i = 0; i < 8; ++i) v[i] = __fmul_rn((float)fy[0][n][i], w[i]);
+                    two_terms(v, fy[0][n], fy[1][n]);
                 }
             }
 #pragma unroll
             for (int m = 0; m < CM; ++m) {
                 const i32x2 b = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds32x2 *)(st + (c_lane ^ (unsigned)(m << 4))));
-                union { uint32_t u[4]; bf16x8 v; } fc;
+                float v[8];
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
                     const int x = b[h >> 1] >> (16 * (h & 1));
-                    fc.u[h] = __builtin_amdgcn_perm(__float_as_uint((float)(int8_t)(x >> 8)), __float_as_uint((float)(int8_t)x), 0x07060302u);
+                    v[2 * h] = (float)(int8_t)x;
+                    v[2 * h + 1] = (float)(int8_t)(x >> 8);
+                }
+                bf16x8 fc[2];
+                if (Sh::SCALE_CODES) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], w[i]);
+                    two_terms(v, fc[0], fc[1]);
+                } else {
+                    fc[0] = upper_halves(v);
                 }
 #pragma unroll
                 for (int term = 1; term >= 0; --term)
 #pragma unroll
-                    for (int n = 0; n < CN; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fc.v, fy[term][n], acc[m][n], 0, 0, 0);
+                    for (int n = 0; n < CN; ++n)
+                        acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fc[Sh::SCALE_CODES ? term : 0], fy[Sh::SCALE_CODES ? 0 : term][n], acc[m][n], 0, 0, 0);
             }
             slot = slot + 1 == NS ? 0 : slot + 1;
         }
@@ -477,25 +513,29 @@ checkpoint_grad_ring_kernel(GradArgs a) {
 }
 
 // The planes of the examples of more than one segment, added in the order of their tokens.
-template <class Out>
+template <class Out, int W>
 __global__ void __launch_bounds__(256)
 checkpoint_join_kernel(GradArgs a) {
     const int64_t e = blockIdx.y, size = (int64_t)a.R * a.D, p0 = phi(a, e, a.chunk);
     int64_t p1 = phi(a, e + 1, a.chunk);
     if (p1 > a.segments) p1 = a.segments;
     if (p1 - p0 < 2) return;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
-        float s = a.planes[p0 * size + i];
-        for (int64_t p = p0 + 1; p < p1; ++p) s = __fadd_rn(s, a.planes[p * size + i]);
-        Out *out = (Out *)a.G + e * a.ldG + i;
-        if (sizeof(Out) == 2) *out = (Out)bf16_bits(s); else *out = (Out)s;
+    typedef __attribute__((ext_vector_type(W))) float fw;
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * W; i < size; i += (int64_t)gridDim.x * 256 * W) {
+        fw s = *(const fw *)(a.planes + p0 * size + i);
+#pragma unroll 4
+        for (int64_t p = p0 + 1; p < p1; ++p) s += *(const fw *)(a.planes + p * size + i);
+        Out x[W];
+#pragma unroll
+        for (int u = 0; u < W; ++u) x[u] = sizeof(Out) == 2 ? (Out)bf16_bits(((const float *)&s)[u]) : (Out)((const float *)&s)[u];
+        __builtin_memcpy((Out *)a.G + e * a.ldG + i, x, sizeof x);
     }
 }
 
 // ---- Many rows of R (a layer's own weights): the products are the bound, so that the activations are formed once, as bfloat16 rows of
 // tokens, and the tiles of product.h multiply them with the gradients.  fp32 results take the activations as the sum of two bfloat16
 // numbers (exact: a code times its step has 15 bits), bfloat16 ones rounded once, which is half the products.
-// A workgroup 64 tokens of an example (the last ones of it with zeros behind them): block e + offset[e] / 64 and on, TERMS times 64 rows each.
+// Workgroups take 64 tokens of an example (the last ones of it with zeros behind them): block e + offset[e] / 64 and on, TERMS times 64 rows each.
 template <int TERMS>
 __global__ void __launch_bounds__(256)
 checkpoint_expand_kernel(GradArgs a, uint16_t *out, int64_t ld) {
@@ -503,7 +543,7 @@ checkpoint_expand_kernel(GradArgs a, uint16_t *out, int64_t ld) {
     if (e < 0) return;
     const int64_t o1 = offset_at(a, e + 1), t0 = offset_at(a, e) + 64 * (j - phi(a, e, 64));
     out += j * TERMS * 64 * ld;
-    for (int64_t i = threadIdx.x; i < 64 * (ld / 8); i += 256) {
+    for (int64_t i = (int64_t)blockIdx.y * 256 + threadIdx.x; i < 64 * (ld / 8); i += (int64_t)gridDim.y * 256) {
         const int64_t r = i / (ld / 8), c = (i - r * (ld / 8)) * 8, t = t0 + r, left = t < o1 ? a.D - c : 0;
         const int8_t *in = a.codes + t * a.ldC + c;
         int8_t q[8];
@@ -566,16 +606,16 @@ static qless_status launch_many(const GradArgs &a, hipStream_t st) {
     if (blocks > 0x7FFFFFFF / (64 * TERMS)) return QLESS_ERR_UNSUPPORTED;
     const ProductArgs p{ProductOperand{x, ld * 2, ld * 2, blocks * 64 * TERMS}, ProductOperand{a.dY, a.ldY * 2, (int64_t)a.R * 2, 0},
                         a.R, a.T, nullptr, nullptr, (a.D + 255) / 256, (int32_t)a.n, a.offsets};
-    hipLaunchKernelGGL(checkpoint_expand_kernel<TERMS>, dim3((unsigned)blocks), dim3(256), 0, st, a, x, ld);
+    hipLaunchKernelGGL(checkpoint_expand_kernel<TERMS>, dim3((unsigned)blocks, (unsigned)((ld + 127) / 128)), dim3(256), 0, st, a, x, ld);
     const qless_status rc = launch_product<GradTile, ACROSS, ACROSS, GradStore<Out>, TERMS>(p, typename GradStore<Out>::Args{(Out *)a.G, a.ldG, a.R, a.D}, st);
     return rc == QLESS_OK ? launch_status() : rc;
 }
 
-// Tokens of a segment: two segments for each of the two workgroups of a compute unit, if all were full (the longest example would keep
-// few of them busy for long), but none so short that its plane (written and read, 8 R bytes per column) costs more than its codes.
+// Tokens of a segment: one for each of the two workgroups of a compute unit, if all were full (the longest example would keep few of
+// them busy for long: rank 16, 64 ragged examples of 32768 tokens 64 us in segments of 2048, 48 of 512, 52 of 256), but none so short that its plane (written and read, 8 R bytes per column) costs more than its codes.
 static int64_t grad_chunk(int64_t T, int32_t R, int32_t D) {
     const int64_t tiles = ((R + 127) / 128) * ((D + 4 * kGroup - 1) / (4 * kGroup)) * (R > 64 ? 2 : 1);
-    int64_t chunk = T * tiles / (4 * (int64_t)compute_units());
+    int64_t chunk = T * tiles / (2 * (int64_t)compute_units());
     if (chunk < 8 * (int64_t)R) chunk = 8 * (int64_t)R;
     if (chunk < 128) chunk = 128;
     if (chunk >= T) chunk = T + 1;
@@ -586,9 +626,11 @@ static int64_t grad_segments(int64_t T, int64_t n, int64_t chunk) { return n + T
 template <class Out>
 static void launch_join(const GradArgs &a, hipStream_t st) {
     if (a.segments <= a.n) return;
-    int64_t bx = ((int64_t)a.R * a.D + 1023) / 1024;
+    const int64_t size = (int64_t)a.R * a.D;
+    int64_t bx = (size + 1023) / 1024;
     if (bx > 1024) bx = 1024;
-    hipLaunchKernelGGL(checkpoint_join_kernel<Out>, dim3((unsigned)bx, (unsigned)a.n), dim3(256), 0, st, a);
+    if (size % 4 == 0) hipLaunchKernelGGL((checkpoint_join_kernel<Out, 4>), dim3((unsigned)bx, (unsigned)a.n), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((checkpoint_join_kernel<Out, 1>), dim3((unsigned)bx, (unsigned)a.n), dim3(256), 0, st, a);
 }
 template <int RT, class Y, int TERMS, class Out>
 static qless_status launch_grad(GradArgs a, hipStream_t st) {
