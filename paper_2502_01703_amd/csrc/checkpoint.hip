@@ -138,10 +138,10 @@ checkpoint_read_kernel(const int8_t *codes, int64_t ldC, const float *step, int6
 // ---------------------------------------------------------------------------------------------------------------------------
 // Weight gradients per example: G_e[r][d] = sum over the tokens t of example e of dY[t][r] code[t][d] step[t][d / 128].
 //
-// The tokens are cut at the multiples of `chunk` and at the examples' ends.  With phi(e) = e + floor(offset[e] / chunk), example e
-// owns the segments phi(e) .. phi(e + 1) - 1 (the last may be empty), which any workgroup finds by bisection, with no list of
-// them in memory; an example of one segment is written at once, the others' segments leave fp32 planes that a second kernel adds in
-// their order.
+// An example longer than `chunk` tokens is cut into segments of that many.  With phi(e) = e + floor(offset[e] / chunk), the numbers
+// phi(e) .. phi(e + 1) - 1 suffice for those of example e (one may be left over), so that any workgroup finds its segment by a search
+// over the offsets, with no list of them in memory; an example of one segment is written at once, the others' segments leave fp32
+// planes that a second kernel adds in their order.
 struct GradArgs {
     const void *dY; int64_t ldY;
     const int8_t *codes; int64_t ldC;
@@ -158,33 +158,43 @@ __device__ inline int64_t offset_at(const GradArgs &a, int64_t e) {      // neve
     const int64_t o = a.offsets[e];
     return o < 0 ? 0 : (o > a.T ? a.T : o);
 }
+__device__ inline int64_t readlane64(int64_t x, int lane) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)x >> 32), lane);
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
 __device__ inline int64_t phi(const GradArgs &a, int64_t e, int64_t chunk) { return e + offset_at(a, e) / chunk; }
 // The example with phi(example) <= j < phi(example + 1), or -1; the whole wavefront asks, 64 examples at a time (a search by halves is a
 // chain of loads as long as a few stages of the work itself).
-__device__ inline int64_t find_example(const GradArgs &a, int64_t j, int64_t chunk) {
+__device__ inline int64_t find_example(const GradArgs &a, int64_t j, int64_t chunk, int64_t &o0, int64_t &o1) {
     const int lane = threadIdx.x & 63;
     int64_t lo = 0, hi = a.n;                              // phi(lo) <= j < phi(hi), once both are known
     bool inside = j < phi(a, a.n, chunk);
     for (;;) {
-        const int64_t step = (hi - lo + 63) / 64, e = lo + lane * step;
-        const uint64_t below = __ballot(e < hi && phi(a, e < hi ? e : lo, chunk) <= j);
+        const int64_t step = (hi - lo + 63) / 64, e = lo + lane * step < hi ? lo + lane * step : hi - 1;
+        const int64_t first = offset_at(a, e), second = offset_at(a, e + 1);
+        const uint64_t below = __ballot(lo + lane * step < hi && e + first / chunk <= j);
         if (below == 0) inside = false;                    // j < phi(0)
         if (!inside) return -1;
         const int at = 63 - __clzll((long long)below);
         lo += at * step;
-        if (step == 1) break;
+        if (step == 1) {
+            o0 = readlane64(first, at);
+            o1 = readlane64(second, at);
+            break;
+        }
         hi = lo + step < hi ? lo + step : hi;
     }
     return (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)lo);
 }
 __device__ inline bool find_segment(const GradArgs &a, int64_t j, Segment &s) {
-    s.e = find_example(a, j, a.chunk);
+    int64_t o0, o1;
+    s.e = find_example(a, j, a.chunk, o0, o1);
     if (s.e < 0) return false;
-    const int64_t o0 = offset_at(a, s.e), o1 = offset_at(a, s.e + 1), i = j - (s.e + o0 / a.chunk);
-    const int64_t c0 = (o0 / a.chunk + i) * a.chunk, c1 = c0 + a.chunk;
-    s.lo = c0 > o0 ? c0 : o0;
-    s.hi = c1 < o1 ? c1 : o1;
-    s.whole = o0 / a.chunk == o1 / a.chunk;
+    const int64_t i = j - (s.e + o0 / a.chunk);
+    s.lo = o0 + i * a.chunk;
+    if (i > 0 && s.lo >= o1) return false;
+    s.hi = s.lo + a.chunk < o1 ? s.lo + a.chunk : o1;
+    s.whole = o1 - o0 <= a.chunk;
     return true;
 }
 
@@ -332,10 +342,10 @@ checkpoint_grad_kernel(GradArgs a) {
 // Rows of 128 codes are exchanged by 16-byte chunks, rows of gradients by 32-byte pieces, so that the eight (four) rows of each of two
 // lane groups lie in different banks.
 template <int RT> struct GradRing {
-    static constexpr int GROUPS = RT >= 128 ? 2 : 4, KT = 32, NS = 4, CM = GROUPS * 2, CN = RT / 16;
-    static constexpr int CODES = GROUPS * KT * 128, Y = KT * RT * 2, STAGE = CODES + Y + 1024, LDS = NS * STAGE;
+    static constexpr int NW = 4, SPLIT = RT >= 128 ? 2 : 1, GROUPS = NW / SPLIT, KT = 32, NS = 4, CM = 8 / SPLIT, CN = RT / 16;     // SPLIT: wavefronts of a group
+    static constexpr int CODES = GROUPS * KT * 128, Y = KT * RT * 2, STAGE = CODES + Y + NW * 256, LDS = NS * STAGE;
     static constexpr bool SCALE_CODES = RT >= 128;         // the side with fewer fragments takes the steps
-    static constexpr int UC = GROUPS, YQ = Y / 1024, UY = (YQ + 3) / 4, U = UC + UY + 1;
+    static constexpr int UC = 4 / SPLIT, YQ = Y / 1024, UY = (YQ + NW - 1) / NW, U = UC + UY + 1;
     static_assert((NS - 2) * U < 64, "vmcnt is a 6-bit counter");
 };
 __device__ inline void global_to_lds4(const void *base, unsigned lane_off, unsigned lds_addr) {      // lane L: LDS bytes [lds_addr + 4 L, + 4)
@@ -358,7 +368,7 @@ __device__ inline void two_terms(const float (&v)[8], bf16x8 &first, bf16x8 &sec
 }
 
 template <int RT, class Out>
-__global__ void __launch_bounds__(256, 2)
+__global__ void __launch_bounds__(64 * GradRing<RT>::NW, 2)
 checkpoint_grad_ring_kernel(GradArgs a) {
     typedef GradRing<RT> Sh;
     constexpr int GROUPS = Sh::GROUPS, KT = Sh::KT, NS = Sh::NS, CM = Sh::CM, CN = Sh::CN, YL = RT / 8;      // YL: lanes of a row of gradients
@@ -370,7 +380,7 @@ checkpoint_grad_ring_kernel(GradArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, quad = lane >> 4;
     const unsigned lds0 = (unsigned)(uintptr_t)((__attribute__((address_space(3))) unsigned char *)smem);
     const int groups = (a.D + kGroup - 1) / kGroup, r0 = rt * RT;
-    const int gl = RT >= 128 ? wave >> 1 : wave, c0 = RT >= 128 ? (wave & 1) * 64 : 0, g = gt + gl < groups ? gt + gl : groups - 1;
+    const int gl = wave / Sh::SPLIT, c0 = wave % Sh::SPLIT * 64, g = gt + gl < groups ? gt + gl : groups - 1;
     auto yswizzle = [](int k) { return RT >= 128 ? k & 7 : RT == 64 ? (k >> 1) & 3 : RT == 32 ? (k >> 2) & 1 : 0; };
     auto swizzle = [](int k) { return ((k >> 1) & 3) | ((k >> 4) & 1) << 2; };
 
@@ -516,10 +526,10 @@ checkpoint_grad_ring_kernel(GradArgs a) {
 template <class Out, int W>
 __global__ void __launch_bounds__(256)
 checkpoint_join_kernel(GradArgs a) {
-    const int64_t e = blockIdx.y, size = (int64_t)a.R * a.D, p0 = phi(a, e, a.chunk);
-    int64_t p1 = phi(a, e + 1, a.chunk);
+    const int64_t e = blockIdx.y, size = (int64_t)a.R * a.D, p0 = phi(a, e, a.chunk), length = offset_at(a, e + 1) - offset_at(a, e);
+    if (length <= a.chunk) return;
+    int64_t p1 = p0 + (length + a.chunk - 1) / a.chunk;
     if (p1 > a.segments) p1 = a.segments;
-    if (p1 - p0 < 2) return;
     typedef __attribute__((ext_vector_type(W))) float fw;
     for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * W; i < size; i += (int64_t)gridDim.x * 256 * W) {
         fw s = *(const fw *)(a.planes + p0 * size + i);
@@ -539,9 +549,10 @@ checkpoint_join_kernel(GradArgs a) {
 template <int TERMS>
 __global__ void __launch_bounds__(256)
 checkpoint_expand_kernel(GradArgs a, uint16_t *out, int64_t ld) {
-    const int64_t j = blockIdx.x, e = find_example(a, j, 64);
+    int64_t o0, o1;
+    const int64_t j = blockIdx.x, e = find_example(a, j, 64, o0, o1);
     if (e < 0) return;
-    const int64_t o1 = offset_at(a, e + 1), t0 = offset_at(a, e) + 64 * (j - phi(a, e, 64));
+    const int64_t t0 = o0 + 64 * (j - (e + o0 / 64));
     out += j * TERMS * 64 * ld;
     for (int64_t i = (int64_t)blockIdx.y * 256 + threadIdx.x; i < 64 * (ld / 8); i += (int64_t)gridDim.y * 256) {
         const int64_t r = i / (ld / 8), c = (i - r * (ld / 8)) * 8, t = t0 + r, left = t < o1 ? a.D - c : 0;
@@ -649,7 +660,7 @@ static qless_status launch_ring(GradArgs a, hipStream_t st) {
     a.dtiles = (a.D + kGroup * GradRing<RT>::GROUPS - 1) / (kGroup * GradRing<RT>::GROUPS);
     const int64_t grid = a.segments * a.rtiles * a.dtiles;
     if (grid > 0x7FFFFFFF) return QLESS_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((checkpoint_grad_ring_kernel<RT, Out>), dim3((unsigned)grid), dim3(256), GradRing<RT>::LDS, st, a);
+    hipLaunchKernelGGL((checkpoint_grad_ring_kernel<RT, Out>), dim3((unsigned)grid), dim3(64 * GradRing<RT>::NW), GradRing<RT>::LDS, st, a);
     launch_join<Out>(a, st);
     return launch_status();
 }
