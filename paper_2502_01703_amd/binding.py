@@ -393,27 +393,26 @@ CHECKPOINT_GROUP = 128                  # QLESS_CHECKPOINT_GROUP of qless.h: col
 
 
 def _rows(t, dtype=None):
-    """Checks a device matrix whose rows are dense, and returns its leading dimension."""
-    assert t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1) and (dtype is None or t.dtype == dtype)
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+    """Checks a matrix whose rows are dense, and returns its leading dimension."""
+    (n, d), (ld, one) = t.shape, t.stride()
+    assert (one == 1 or d == 1) and (dtype is None or t.dtype == dtype)
+    return ld if n > 1 else max(d, ld)
 
 
-class _On:
-    """The device of a call's tensors as the current one: kernels and workspaces belong there."""
+# the current device's number itself, as above
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
-    def __init__(self, *tensors):
-        self.device = tensors[0].device
-        for t in tensors:
-            assert t is None or t.device == self.device, "all tensors of a call lie on one device"
 
-    def __enter__(self):
-        self.before = torch.cuda.current_device()
-        if self.device.index != self.before:
-            torch.cuda.set_device(self.device)
-
-    def __exit__(self, *_):
-        if self.device.index != self.before:
-            torch.cuda.set_device(self.before)
+def _elsewhere(call, first, *others):
+    """Where the tensors of a call lie on another device than the current one: the call made there, in a tuple; else None."""
+    device = first.get_device()
+    assert device >= 0, "device tensors"
+    for t in others:
+        assert t is None or t.get_device() == device, "all tensors of a call lie on one device"
+    if device == _current_device():
+        return None
+    with torch.cuda.device(device):
+        return (call(),)
 
 
 def token_loss_workspace(T, D, V, want_dH=True, want_dW=False):
@@ -423,56 +422,67 @@ def token_loss_workspace(T, D, V, want_dH=True, want_dW=False):
 def token_loss(H, W, target, weight=None, want_dH=True, want_dW=False, dH=None, dW=None, ws=None):
     """qless_token_loss: last hidden states H [T, D] and head W [V, D] (bf16, row strides free), targets int64 [T] (outside
     [0, V): left out), weights fp32 [T] or None -> (nll [T], lse [T], dH [T, D] or None, dW [V, D] or None)."""
-    ldH, ldW = _rows(H), _rows(W)
+    there = _elsewhere(lambda: token_loss(H, W, target, weight, want_dH, want_dW, dH, dW, ws), H, W, target, weight, dH, dW, ws)
+    if there:
+        return there[0]
+    ldH, ldW = _rows(H), _rows(W, H.dtype)
     (T, D), V = H.shape, W.shape[0]
-    assert W.shape[1] == D and W.dtype == H.dtype
-    assert target.is_cuda and target.dtype == torch.int64 and target.shape == (T,) and target.is_contiguous()
+    assert W.shape[1] == D and target.dtype == torch.int64 and target.shape == (T,) and target.is_contiguous()
     assert weight is None or (weight.dtype == torch.float32 and weight.shape == (T,) and weight.is_contiguous())
-    with _On(H, W, target, weight, dH, dW, ws):
-        nll = torch.empty(T, dtype=torch.float32, device=H.device)
-        lse = torch.empty(T, dtype=torch.float32, device=H.device)
-        if want_dH and dH is None:
-            dH = torch.empty(T, D, dtype=H.dtype, device=H.device)
-        if want_dW and dW is None:
-            dW = torch.empty(V, D, dtype=W.dtype, device=H.device)
-        assert dH is None or (dH.shape == H.shape and dH.dtype == H.dtype)
-        assert dW is None or (dW.shape == W.shape and dW.dtype == W.dtype)
-        w = _ws(token_loss_workspace(T, D, V, dH is not None, dW is not None), H.device) if ws is None else ws
-        _check(lib().qless_token_loss(H.data_ptr(), ldH, W.data_ptr(), ldW, _dtype_code(H), T, D, V, target.data_ptr(),
-                                      weight.data_ptr() if weight is not None else None, nll.data_ptr(), lse.data_ptr(),
-                                      dH.data_ptr() if dH is not None else None, _rows(dH) if dH is not None else 0,
-                                      dW.data_ptr() if dW is not None else None, _rows(dW) if dW is not None else 0,
-                                      w.data_ptr(), w.numel(), _stream()), "qless_token_loss")
+    nll = torch.empty(T, dtype=torch.float32, device=H.device)
+    lse = torch.empty(T, dtype=torch.float32, device=H.device)
+    if want_dH and dH is None:
+        dH = torch.empty(T, D, dtype=H.dtype, device=H.device)
+    if want_dW and dW is None:
+        dW = torch.empty(V, D, dtype=W.dtype, device=H.device)
+    assert dH is None or dH.shape == H.shape
+    assert dW is None or dW.shape == W.shape
+    w = _ws(token_loss_workspace(T, D, V, dH is not None, dW is not None), H.device) if ws is None else ws
+    _check(lib().qless_token_loss(H.data_ptr(), ldH, W.data_ptr(), ldW, _dtype_code(H), T, D, V, target.data_ptr(),
+                                  weight.data_ptr() if weight is not None else None, nll.data_ptr(), lse.data_ptr(),
+                                  dH.data_ptr() if dH is not None else None, _rows(dH, H.dtype) if dH is not None else 0,
+                                  dW.data_ptr() if dW is not None else None, _rows(dW, H.dtype) if dW is not None else 0,
+                                  w.data_ptr(), w.numel(), _stream()), "qless_token_loss")
     return nll, lse, dH, dW
 
 
 def checkpoint8(X, codes=None, step=None):
     """qless_checkpoint8: activations X [T, D] (fp32 or bf16, row stride free) -> (codes int8 [T, D],
     step fp32 [T, ceil(D / 128)])."""
+    there = _elsewhere(lambda: checkpoint8(X, codes, step), X, codes, step)
+    if there:
+        return there[0]
     ldX = _rows(X)
     T, D = X.shape
-    with _On(X, codes, step):
-        if codes is None:
-            codes = torch.empty(T, D, dtype=torch.int8, device=X.device)
-        if step is None:
-            step = torch.empty(T, -(-D // CHECKPOINT_GROUP), dtype=torch.float32, device=X.device)
-        assert codes.shape == X.shape and step.shape == (T, -(-D // CHECKPOINT_GROUP))
-        _check(lib().qless_checkpoint8(X.data_ptr(), _dtype_code(X), T, D, ldX, codes.data_ptr(), _rows(codes, torch.int8),
-                                       step.data_ptr(), _rows(step, torch.float32), _stream()), "qless_checkpoint8")
+    G = -(-D // CHECKPOINT_GROUP)
+    if codes is None:
+        codes, ldC = torch.empty((T, D), dtype=torch.int8, device=X.device), D
+    else:
+        assert codes.shape == X.shape
+        ldC = _rows(codes, torch.int8)
+    if step is None:
+        step, ldS = torch.empty((T, G), dtype=torch.float32, device=X.device), G
+    else:
+        assert step.shape == (T, G)
+        ldS = _rows(step, torch.float32)
+    _check(lib().qless_checkpoint8(X.data_ptr(), _dtype_code(X), T, D, ldX, codes.data_ptr(), ldC, step.data_ptr(), ldS, _stream()),
+           "qless_checkpoint8")
     return codes, step
 
 
 def checkpoint8_read(codes, step, dtype=torch.bfloat16, out=None):
     """qless_checkpoint8_read: codes [T, D] and steps -> the activations [T, D] in fp32 or bf16."""
+    there = _elsewhere(lambda: checkpoint8_read(codes, step, dtype, out), codes, step, out)
+    if there:
+        return there[0]
     ldC, ldS = _rows(codes, torch.int8), _rows(step, torch.float32)
     T, D = codes.shape
     assert step.shape == (T, -(-D // CHECKPOINT_GROUP))
-    with _On(codes, step, out):
-        if out is None:
-            out = torch.empty(T, D, dtype=dtype, device=codes.device)
-        assert out.shape == codes.shape
-        _check(lib().qless_checkpoint8_read(codes.data_ptr(), ldC, step.data_ptr(), ldS, T, D, out.data_ptr(), _dtype_code(out),
-                                            _rows(out), _stream()), "qless_checkpoint8_read")
+    if out is None:
+        out = torch.empty((T, D), dtype=dtype, device=codes.device)
+    assert out.shape == codes.shape
+    _check(lib().qless_checkpoint8_read(codes.data_ptr(), ldC, step.data_ptr(), ldS, T, D, out.data_ptr(), _dtype_code(out),
+                                        _rows(out), _stream()), "qless_checkpoint8_read")
     return out
 
 
@@ -483,17 +493,19 @@ def checkpoint8_grad_workspace(T, n, R, D):
 def checkpoint8_grad(dY, codes, step, offsets, dtype=torch.float32, out=None, ws=None):
     """qless_checkpoint8_grad: dY [T, R] and a checkpointed input [T, D], examples [offsets[e], offsets[e + 1]) (device, int64) ->
     G [n, R, D], or into `out` [n, R * D] (fp32 or bf16, row stride free: a slice of the rows to project)."""
+    there = _elsewhere(lambda: checkpoint8_grad(dY, codes, step, offsets, dtype, out, ws), dY, codes, step, offsets, out, ws)
+    if there:
+        return there[0]
     ldY, ldC, ldS = _rows(dY), _rows(codes, torch.int8), _rows(step, torch.float32)
     T, R = dY.shape
     D = codes.shape[1]
     n = offsets.numel() - 1
     assert codes.shape[0] == T and step.shape == (T, -(-D // CHECKPOINT_GROUP))
-    assert offsets.is_cuda and offsets.dtype == torch.int64 and offsets.dim() == 1 and offsets.is_contiguous() and n >= 0
-    with _On(dY, codes, step, offsets, out, ws):
-        G = torch.empty(n, R * D, dtype=dtype, device=dY.device) if out is None else out
-        assert G.shape == (n, R * D)
-        w = _ws(checkpoint8_grad_workspace(T, n, R, D), dY.device) if ws is None else ws
-        _check(lib().qless_checkpoint8_grad(dY.data_ptr(), _dtype_code(dY), ldY, R, codes.data_ptr(), ldC, step.data_ptr(), ldS, D, T,
-                                            offsets.data_ptr(), n, G.data_ptr(), _dtype_code(G), _rows(G),
-                                            w.data_ptr(), w.numel(), _stream()), "qless_checkpoint8_grad")
+    assert offsets.dtype == torch.int64 and offsets.dim() == 1 and offsets.is_contiguous() and n >= 0
+    G = torch.empty((n, R * D), dtype=dtype, device=dY.device) if out is None else out
+    assert G.shape == (n, R * D)
+    w = _ws(checkpoint8_grad_workspace(T, n, R, D), dY.device) if ws is None else ws
+    _check(lib().qless_checkpoint8_grad(dY.data_ptr(), _dtype_code(dY), ldY, R, codes.data_ptr(), ldC, step.data_ptr(), ldS, D, T,
+                                        offsets.data_ptr(), n, G.data_ptr(), _dtype_code(G), _rows(G),
+                                        w.data_ptr(), w.numel(), _stream()), "qless_checkpoint8_grad")
     return G.view(n, R, D) if out is None else G

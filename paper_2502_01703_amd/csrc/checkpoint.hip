@@ -85,53 +85,82 @@ __device__ inline int nearest_code(float x, float s, float inv) {
     return (int)q;
 }
 
-// 16 lanes a group, eight columns a lane.  Bound: memory, read once and written once.
+// A workgroup takes kItems consecutive groups, 16 lanes a group and eight columns a lane, kPer of them on their way together.  One division
+// per workgroup finds its first row; the lanes' own are of 32 bits (one of 64 bits per group took as long as the memory).
+// Bound: memory, read once and written once.
+constexpr int kPer = 2, kItems = 16 * kPer;
+struct GroupPlace { int64_t t; int g; };
+__device__ inline GroupPlace group_place(int64_t first, int local, int32_t groups) {       // first: uniform
+    const int64_t t0 = first / groups;
+    const unsigned at = (unsigned)(first - t0 * groups) + (unsigned)local, up = at / (unsigned)groups;
+    return GroupPlace{t0 + up, (int)(at - up * (unsigned)groups)};
+}
+
 template <class T>
 __global__ void __launch_bounds__(256)
 checkpoint_write_kernel(const T *X, int64_t rows, int32_t D, int64_t ldX, int32_t groups, int8_t *codes, int64_t ldC, float *step, int64_t ldS) {
-    const int64_t total = rows * groups, stride = (int64_t)gridDim.x * 16;
-    for (int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); i < total; i += stride) {
-        const int64_t t = i / groups;
-        const int g = (int)(i - t * groups), c = g * kGroup + (threadIdx.x & 15) * 8;
-        float x[8];
-        Eight<T>::load(X + t * ldX + c, D - c, x);
+    const int64_t total = rows * groups, first = (int64_t)blockIdx.x * kItems;
+    const int col = (threadIdx.x & 15) * 8;
+    float x[kPer][8];
+    GroupPlace at[kPer];
+    int left[kPer];
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+        const int local = u * 16 + (threadIdx.x >> 4);
+        at[u] = group_place(first, local, groups);
+        const int c = at[u].g * kGroup + col;
+        left[u] = first + local < total ? D - c : 0;
+        Eight<T>::load(X + at[u].t * ldX + c, left[u], x[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
         uint32_t top = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[u][j]) & 0x7FFFFFFFu);
         top = row_max(top);
         const float s = group_step(top);
         const bool plain = top != 0 && top < 0x7F800000u;
         const float inv = plain ? __fdiv_rn(1.0f, s) : 0.0f;
         int8_t q[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) q[j] = plain ? (int8_t)nearest_code(x[j], s, inv) : (int8_t)0;
-        int8_t *out = codes + t * ldC + c;
-        if (D - c >= 8) __builtin_memcpy(out, q, 8);
+        for (int j = 0; j < 8; ++j) q[j] = plain ? (int8_t)nearest_code(x[u][j], s, inv) : (int8_t)0;
+        int8_t *out = codes + at[u].t * ldC + at[u].g * kGroup + col;
+        if (left[u] >= 8) __builtin_memcpy(out, q, 8);
         else
 #pragma unroll
-            for (int j = 0; j < 8; ++j) if (j < D - c) out[j] = q[j];
-        if ((threadIdx.x & 15) == 0) step[t * ldS + g] = s;
+            for (int j = 0; j < 8; ++j) if (j < left[u]) out[j] = q[j];
+        if (col == 0 && left[u] > 0) step[at[u].t * ldS + at[u].g] = s;
     }
 }
 
 template <class T>
 __global__ void __launch_bounds__(256)
 checkpoint_read_kernel(const int8_t *codes, int64_t ldC, const float *step, int64_t ldS, int64_t rows, int32_t D, int32_t groups, T *X, int64_t ldX) {
-    const int64_t total = rows * groups, stride = (int64_t)gridDim.x * 16;
-    for (int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); i < total; i += stride) {
-        const int64_t t = i / groups;
-        const int g = (int)(i - t * groups), c = g * kGroup + (threadIdx.x & 15) * 8, left = D - c;
-        const int8_t *in = codes + t * ldC + c;
-        int8_t q[8];
-        if (left >= 8) __builtin_memcpy(q, in, 8);
+    const int64_t total = rows * groups, first = (int64_t)blockIdx.x * kItems;
+    const int col = (threadIdx.x & 15) * 8;
+    int8_t q[kPer][8];
+    float s[kPer];
+    GroupPlace at[kPer];
+    int left[kPer];
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+        const int local = u * 16 + (threadIdx.x >> 4);
+        at[u] = group_place(first, local, groups);
+        const int c = at[u].g * kGroup + col;
+        left[u] = first + local < total ? D - c : 0;
+        const int8_t *in = codes + at[u].t * ldC + c;
+        if (left[u] >= 8) __builtin_memcpy(q[u], in, 8);
         else
 #pragma unroll
-            for (int j = 0; j < 8; ++j) q[j] = j < left ? in[j] : (int8_t)0;
-        const float s = step[t * ldS + g];
+            for (int j = 0; j < 8; ++j) q[u][j] = j < left[u] ? in[j] : (int8_t)0;
+        s[u] = left[u] > 0 ? step[at[u].t * ldS + at[u].g] : 0.0f;
+    }
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
         float x[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = __fmul_rn((float)q[j], s);
-        Eight<T>::store(X + t * ldX + c, left, x);
+        for (int j = 0; j < 8; ++j) x[j] = __fmul_rn((float)q[u][j], s[u]);
+        Eight<T>::store(X + at[u].t * ldX + at[u].g * kGroup + col, left[u], x);
     }
 }
 
@@ -682,10 +711,7 @@ static qless_status launch_grad_rows(const GradArgs &a, hipStream_t st) {
 static bool checkpoint_shape_ok(int64_t T, int32_t D, int64_t ldX, int64_t ldC, int64_t ldS) {
     return T >= 0 && D >= 1 && (T <= 1 || (ldX >= D && ldC >= D && ldS >= (D + (int64_t)kGroup - 1) / kGroup));
 }
-static unsigned checkpoint_grid(int64_t T, int32_t groups) {
-    const int64_t blocks = (T * groups + 15) / 16;
-    return (unsigned)(blocks < 4096 ? blocks : 4096);
-}
+static int64_t checkpoint_grid(int64_t T, int32_t groups) { return (T * groups + kItems - 1) / kItems; }
 
 }  // namespace qless
 
@@ -697,11 +723,12 @@ extern "C" qless_status qless_checkpoint8(const void *X, qless_dtype dt, int64_t
     if (T == 0) return QLESS_OK;
     if (!X || !codes || !step) return QLESS_ERR_INVALID_ARG;
     const int32_t groups = (D + kGroup - 1) / kGroup;
+    if (T > ((int64_t)1 << 40) / groups || checkpoint_grid(T, groups) > 0x7FFFFFFF) return QLESS_ERR_UNSUPPORTED;
     const hipStream_t st = (hipStream_t)stream;
     if (dt == QLESS_F32)
-        hipLaunchKernelGGL(checkpoint_write_kernel<float>, dim3(checkpoint_grid(T, groups)), dim3(256), 0, st, (const float *)X, T, D, ldX, groups, codes, ldC, step, ldS);
+        hipLaunchKernelGGL(checkpoint_write_kernel<float>, dim3((unsigned)checkpoint_grid(T, groups)), dim3(256), 0, st, (const float *)X, T, D, ldX, groups, codes, ldC, step, ldS);
     else
-        hipLaunchKernelGGL(checkpoint_write_kernel<uint16_t>, dim3(checkpoint_grid(T, groups)), dim3(256), 0, st, (const uint16_t *)X, T, D, ldX, groups, codes, ldC, step, ldS);
+        hipLaunchKernelGGL(checkpoint_write_kernel<uint16_t>, dim3((unsigned)checkpoint_grid(T, groups)), dim3(256), 0, st, (const uint16_t *)X, T, D, ldX, groups, codes, ldC, step, ldS);
     return launch_status();
 }
 
@@ -713,11 +740,12 @@ extern "C" qless_status qless_checkpoint8_read(const int8_t *codes, int64_t ldC,
     if (T == 0) return QLESS_OK;
     if (!X || !codes || !step) return QLESS_ERR_INVALID_ARG;
     const int32_t groups = (D + kGroup - 1) / kGroup;
+    if (T > ((int64_t)1 << 40) / groups || checkpoint_grid(T, groups) > 0x7FFFFFFF) return QLESS_ERR_UNSUPPORTED;
     const hipStream_t st = (hipStream_t)stream;
     if (dt == QLESS_F32)
-        hipLaunchKernelGGL(checkpoint_read_kernel<float>, dim3(checkpoint_grid(T, groups)), dim3(256), 0, st, codes, ldC, step, ldS, T, D, groups, (float *)X, ldX);
+        hipLaunchKernelGGL(checkpoint_read_kernel<float>, dim3((unsigned)checkpoint_grid(T, groups)), dim3(256), 0, st, codes, ldC, step, ldS, T, D, groups, (float *)X, ldX);
     else
-        hipLaunchKernelGGL(checkpoint_read_kernel<uint16_t>, dim3(checkpoint_grid(T, groups)), dim3(256), 0, st, codes, ldC, step, ldS, T, D, groups, (uint16_t *)X, ldX);
+        hipLaunchKernelGGL(checkpoint_read_kernel<uint16_t>, dim3((unsigned)checkpoint_grid(T, groups)), dim3(256), 0, st, codes, ldC, step, ldS, T, D, groups, (uint16_t *)X, ldX);
     return launch_status();
 }
 
