@@ -11,8 +11,6 @@
 
 namespace qless {
 
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-
 constexpr int kGroup = QLESS_CHECKPOINT_GROUP;
 
 __device__ inline float bf16_value(uint32_t bits) { return __uint_as_float(bits << 16); }
@@ -607,27 +605,18 @@ checkpoint_expand_kernel(GradArgs a, uint16_t *out, int64_t ld) {
 template <class Out> struct GradStore {
     struct Args { Out *G; int64_t ldG; int32_t R, D; };
     template <int FM, int FN>
-    static __device__ inline void run(const Args &a, f32x16 (&acc)[FM][FN], int64_t m, int64_t n, int e, int64_t) {
-        const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
+    static __device__ inline void run(const Args &a, unsigned char *lds, f32x16 (&acc)[FM][FN], int64_t m, int64_t n, int e, int64_t) {
+        by_rows<FM, FN>(lds, acc, [&](int r, int c, f32x4 y) {
+            const int64_t d = m + c;
+            if (n + r >= a.R) return;
+            Out x[4], *out = a.G + e * a.ldG + (n + r) * a.D + d;
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            const int64_t r = n + 32 * j + l32;
-            if (r >= a.R) continue;
-            Out *row = a.G + e * a.ldG + r * a.D;
+            for (int u = 0; u < 4; ++u) x[u] = sizeof(Out) == 2 ? (Out)bf16_bits(y[u]) : (Out)y[u];
+            if (d + 4 <= a.D) __builtin_memcpy(out, x, sizeof x);
+            else
 #pragma unroll
-            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int64_t d = m + 32 * i + 8 * q + 4 * half;
-                    Out x[4];
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) x[u] = sizeof(Out) == 2 ? (Out)bf16_bits(acc[i][j][4 * q + u]) : (Out)acc[i][j][4 * q + u];
-                    if (d + 4 <= a.D) __builtin_memcpy(row + d, x, sizeof x);
-                    else
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) if (d + u < a.D) row[d + u] = x[u];
-                }
-        }
+                for (int u = 0; u < 4; ++u) if (d + u < a.D) out[u] = x[u];
+        });
     }
 };
 typedef ProductShape<256, 256, 2, 4, 2> GradTile;

@@ -12,6 +12,7 @@ namespace qless {
 
 typedef __attribute__((ext_vector_type(4))) short i16x4;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 enum { ALONG = 0, ACROSS = 1 };
@@ -106,10 +107,43 @@ __device__ inline bf16x8 fragment(const unsigned char *stage, unsigned lane_at, 
 template <int MT_, int NT_, int WY_, int WX_, int NS_> struct ProductShape {
     static constexpr int MT = MT_, NT = NT_, WY = WY_, WX = WX_, NS = NS_, NW = WY * WX, FM = MT / WY / 32, FN = NT / WX / 32;
     static constexpr int STAGE = (MT + NT) * 128, LDS = NS * STAGE;
-    static_assert(FM * WY * 32 == MT && FN * WX * 32 == NT && NS >= 2, "whole fragments");
+    static_assert(FM * WY * 32 == MT && FN * WX * 32 == NT && NS >= 2 && NW * FM * 4096 <= LDS, "whole fragments, and room for 32 rows of them");
 };
 
-// Epilogue::run(args, acc, m, n, split, live): acc[i][j][v] is C at m + 32 i + 8 (v / 4) + 4 half + v % 4, n + 32 j + lane % 32.
+// A wavefront's accumulators row by row of n: store(r, c, x) is called for every row r < 32 FN with four columns from c = 4 (lane % (8 FM))
+// on, so that lanes next to each other hold columns next to each other.  32 rows at a time pass through the wavefront's part of `lds`
+// (4 KB per FM), their 16-byte chunks exchanged by the row: the accumulators' own order, 16 to 32 bytes of 32 rows each, took the caches
+// two to four times as many requests.
+template <int FM, int FN, class Store>
+__device__ inline void by_rows(unsigned char *lds, f32x16 (&acc)[FM][FN], Store store) {
+    constexpr int CHUNKS = 8 * FM, ROWS = 64 / CHUNKS;
+    const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31, wave = threadIdx.x >> 6;
+    unsigned char *mine = lds + wave * (FM * 4096);
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                f32x4 x;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) x[u] = acc[i][j][4 * q + u];
+                *(f32x4 *)(mine + l32 * (CHUNKS * 16) + (((8 * i + 2 * q + half) ^ (l32 & (CHUNKS - 1))) << 4)) = x;
+            }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();                   // LDS operations of a wavefront complete in order
+#pragma unroll 8
+        for (int r0 = 0; r0 < 32; r0 += ROWS) {
+            const int r = r0 + lane / CHUNKS, c = lane % CHUNKS;
+            store(32 * j + r, 4 * c, *(const f32x4 *)(mine + r * (CHUNKS * 16) + ((c ^ (r & (CHUNKS - 1))) << 4)));
+        }
+    }
+}
+
+// Epilogue::run(args, lds, acc, m, n, split, live): acc[i][j][v] is C at m + 32 i + 8 (v / 4) + 4 half + v % 4, n + 32 j + lane % 32; lds: the
+// workgroup's, free.
 template <class Sh, int AK, int BK, class Epilogue, int CUTS = 0>
 __global__ void __launch_bounds__(64 * Sh::NW, Sh::NW / 4)
 product_kernel(ProductArgs p, typename Epilogue::Args e) {
@@ -217,7 +251,8 @@ product_kernel(ProductArgs p, typename Epilogue::Args e) {
         }
         wait_vmcnt<0>();                                   // no copy is under way when the workgroup gives its LDS back
     }
-    Epilogue::template run<FM, FN>(e, acc, m0 + ma, n0 + nb, split, n);
+    __syncthreads();                                       // everyone has read the last stage
+    Epilogue::template run<FM, FN>(e, smem, acc, m0 + ma, n0 + nb, split, n);
 }
 
 template <class Sh, int AK, int BK, class Epilogue, int CUTS = 0>

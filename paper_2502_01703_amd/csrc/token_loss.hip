@@ -148,8 +148,7 @@ __device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 template <bool STORE, bool SUM> struct LossStats {
     struct Args { const int32_t *target; float *hit; float2 *part; int64_t Tp, first; int32_t V; float *logits; int64_t ld; };
     template <int FM, int FN>
-    static __device__ inline void run(const Args &a, f32x16 (&acc)[FM][FN], int64_t m, int64_t n, int, int64_t live) {
-        typedef __attribute__((ext_vector_type(4))) float f32x4;
+    static __device__ inline void run(const Args &a, unsigned char *lds, f32x16 (&acc)[FM][FN], int64_t m, int64_t n, int, int64_t live) {
         const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
         const int64_t part = ((STORE ? 0 : a.first) + m) / (32 * FM);
         const int v0 = (int)(a.first + m) + 4 * half, over = a.V - v0;         // entries from here on
@@ -172,17 +171,6 @@ template <bool STORE, bool SUM> struct LossStats {
 #pragma unroll
                     for (int v = 0; v < 16; ++v) acc[i][j][v] = 32 * i + 8 * (v >> 2) + (v & 3) < over ? acc[i][j][v] : -INFINITY;
             }
-            if (STORE && t < live) {
-#pragma unroll
-                for (int i = 0; i < FM; ++i)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        f32x4 x;
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) x[u] = acc[i][j][4 * q + u];
-                        *(f32x4 *)(a.logits + t * a.ld + m + 32 * i + 8 * q + 4 * half) = x;
-                    }
-            }
             float top = acc[0][j][0];
 #pragma unroll
             for (int i = 0; i < FM; ++i)
@@ -200,6 +188,10 @@ template <bool STORE, bool SUM> struct LossStats {
             }
             if (half == 0 && t < live) a.part[part * a.Tp + t] = make_float2(top, sum);
         }
+        if (STORE)
+            by_rows<FM, FN>(lds, acc, [&](int r, int c, f32x4 x) {
+                if (n + r < live) *(f32x4 *)(a.logits + (n + r) * a.ld + m + c) = x;
+            });
     }
 };
 
@@ -207,31 +199,23 @@ template <bool STORE, bool SUM> struct LossStats {
 template <bool FEW> struct LossDelta {
     struct Args { const int32_t *target; const float *lse, *weight; uint16_t *delta; int64_t ld, first; int32_t V; };
     template <int FM, int FN>
-    static __device__ inline void run(const Args &a, f32x16 (&acc)[FM][FN], int64_t m, int64_t n, int, int64_t live) {
-        const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
-#pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            const int64_t t = n + 32 * j + l32;
+    static __device__ inline void run(const Args &a, unsigned char *lds, f32x16 (&acc)[FM][FN], int64_t m, int64_t n, int, int64_t live) {
+        by_rows<FM, FN>(lds, acc, [&](int r, int c, f32x4 z) {
+            const int64_t t = n + r;
             const bool on = t < live;
             const float lse = on ? a.lse[t] : 0.0f, w = on ? a.weight[t] : 0.0f;
-            const int c0 = (int)m + 4 * half, y = on ? a.target[t] - (int)a.first - c0 : -1, over = on ? a.V - (int)a.first - c0 : 0;
-            uint16_t *row = a.delta + t * a.ld + c0;
+            const int c0 = (int)m + c, y = on ? a.target[t] - (int)a.first - c0 : -1, over = on ? a.V - (int)a.first - c0 : 0;
+            uint16_t d[4], rest[4];
 #pragma unroll
-            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    uint16_t d[4], rest[4];
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const int at = 32 * i + 8 * q + u;
-                        const float x = at < over && at != y ? w * __expf(acc[i][j][4 * q + u] - lse) : 0.0f;
-                        d[u] = __builtin_bit_cast(uint16_t, (__bf16)x);
-                        rest[u] = __builtin_bit_cast(uint16_t, (__bf16)(x - __uint_as_float((uint32_t)d[u] << 16)));
-                    }
-                    __builtin_memcpy(__builtin_assume_aligned(row + 32 * i + 8 * q, 8), d, 8);
-                    if (FEW) __builtin_memcpy(__builtin_assume_aligned(row + kFew * a.ld + 32 * i + 8 * q, 8), rest, 8);
-                }
-        }
+            for (int u = 0; u < 4; ++u) {
+                const float x = u < over && u != y ? w * __expf(z[u] - lse) : 0.0f;
+                d[u] = __builtin_bit_cast(uint16_t, (__bf16)x);
+                rest[u] = __builtin_bit_cast(uint16_t, (__bf16)(x - __uint_as_float((uint32_t)d[u] << 16)));
+            }
+            uint16_t *out = a.delta + t * a.ld + c0;
+            __builtin_memcpy(__builtin_assume_aligned(out, 8), d, 8);
+            if (FEW) __builtin_memcpy(__builtin_assume_aligned(out + kFew * a.ld, 8), rest, 8);
+        });
     }
 };
 
@@ -240,28 +224,25 @@ template <bool FEW> struct LossDelta {
 template <bool FEW> struct LossPlane {
     struct Args { float *planes; int64_t Tp, Dp; const float *shrink; };
     template <int FM, int FN>
-    static __device__ inline void run(const Args &a, f32x16 (&acc)[FM][FN], int64_t m, int64_t n, int split, int64_t live) {
-        typedef __attribute__((ext_vector_type(4))) float f32x4;
+    static __device__ inline void run(const Args &a, unsigned char *lds, f32x16 (&acc)[FM][FN], int64_t m, int64_t n, int split, int64_t live) {
         static_assert(!FEW || FN * 32 == 2 * kFew, "both terms in one wavefront");
-        const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
+        if (FEW)
 #pragma unroll
-        for (int j = 0; j < (FEW ? 1 : FN); ++j) {
-            const int64_t t = n + 32 * j + l32;
-            if (t >= live) continue;
-            float *row = a.planes + (split * a.Tp + t) * a.Dp;
-            const float shrink = a.shrink ? a.shrink[t] : 0.0f;
+            for (int i = 0; i < FM; ++i) acc[i][0] += acc[i][FN - 1];
+        auto store = [&](int r, int c, f32x4 x) {
+            const int64_t t = n + r;
+            if (t >= live || m + c >= a.Dp) return;
+            float *out = a.planes + (split * a.Tp + t) * a.Dp + m + c;
+            if (a.shrink) x += *(const f32x4 *)out * a.shrink[t];
+            *(f32x4 *)out = x;
+        };
+        if (FEW) {
+            f32x16 first[FM][1];
 #pragma unroll
-            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int64_t d = m + 32 * i + 8 * q + 4 * half;
-                    if (d >= a.Dp) continue;
-                    f32x4 x;
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) x[u] = FEW ? acc[i][0][4 * q + u] + acc[i][FN - 1][4 * q + u] : acc[i][j][4 * q + u];
-                    if (a.shrink) x += *(const f32x4 *)(row + d) * shrink;
-                    *(f32x4 *)(row + d) = x;
-                }
+            for (int i = 0; i < FM; ++i) first[i][0] = acc[i][0];
+            by_rows<FM, 1>(lds, first, store);
+        } else {
+            by_rows<FM, FN>(lds, acc, store);
         }
     }
 };
@@ -273,7 +254,7 @@ struct LossHead {
         const int32_t *order, *order_target, *start; const float *pull; const uint16_t *H; int64_t Dp;
     };
     template <int FM, int FN>
-    static __device__ inline void run(const Args &a, f32x16 (&acc)[FM][FN], int64_t m, int64_t n, int, int64_t) {
+    static __device__ inline void run(const Args &a, unsigned char *lds, f32x16 (&acc)[FM][FN], int64_t m, int64_t n, int, int64_t) {
         static_assert(FN == 2, "64 entries a wavefront");
         const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
         const int block = __builtin_amdgcn_readfirstlane((int)((a.first + n) / 64));
@@ -295,25 +276,17 @@ struct LossHead {
             };
             if (col < 32) add(0); else add(1);
         }
+        by_rows<FM, FN>(lds, acc, [&](int r, int c, f32x4 y) {
+            const int64_t v = a.first + n + r, d = m + c;
+            if (v >= a.V) return;
+            uint16_t x[4], *out = a.dW + v * a.ld + d;
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            const int64_t v = a.first + n + 32 * j + l32;
-            if (v >= a.V) continue;
-            uint16_t *row = a.dW + v * a.ld;
+            for (int u = 0; u < 4; ++u) x[u] = __builtin_bit_cast(uint16_t, (__bf16)y[u]);
+            if (d + 4 <= a.D) __builtin_memcpy(out, x, 8);
+            else
 #pragma unroll
-            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int64_t d = m + 32 * i + 8 * q + 4 * half;
-                    uint16_t x[4];
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) x[u] = __builtin_bit_cast(uint16_t, (__bf16)acc[i][j][4 * q + u]);
-                    if (d + 4 <= a.D) __builtin_memcpy(row + d, x, 8);
-                    else
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) if (d + u < a.D) row[d + u] = x[u];
-                }
-        }
+                for (int u = 0; u < 4; ++u) if (d + u < a.D) out[u] = x[u];
+        });
     }
 };
 
