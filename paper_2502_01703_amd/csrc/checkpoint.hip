@@ -8,6 +8,8 @@
 // fp32 sums with two matrix products instead of three.  A group with an infinity or a NaN gets the step NaN and codes 0.
 #include "product.h"
 #include "score.h"
+#include <cmath>
+#include <type_traits>
 
 namespace qless {
 
@@ -176,6 +178,7 @@ struct GradArgs {
     const int64_t *offsets;
     int64_t n, T, chunk, segments;
     int32_t R, D, rtiles, dtiles;
+    int32_t Rc, Dc;                                        // columns of dY and codes that may be read: R and D, or more where they are packed
     void *G; int64_t ldG;
     float *planes;                                         // [segments][R][D]
 };
@@ -360,7 +363,7 @@ checkpoint_grad_kernel(GradArgs a) {
     }
 }
 
-// The same for bfloat16 gradients and operands whose rows are whole 16-byte chunks.  A workgroup takes RT rows of R x GROUPS groups, a
+// The same for bfloat16 gradients and operands whose rows are whole 16-byte chunks (or were made so).  A workgroup takes RT rows of R x GROUPS groups, a
 // wavefront of it one group (or half of one); stages of 32 tokens' codes, gradients and steps are copied to a ring of NS in LDS
 // without passing through registers, three of them on their way while one is used: codes stay 8 bits wide until the transposing
 // reads have brought eight tokens of a column into a lane, and the step is multiplied there, into the gradients or, from 128 rows on,
@@ -420,14 +423,14 @@ checkpoint_grad_ring_kernel(GradArgs a) {
         const int q = wave * Sh::UC + u;
         crow[u] = 8 * (q & 3) + (lane >> 3);
         const int at = (gt + (q >> 2)) * kGroup + ((lane & 7) ^ swizzle(crow[u])) * 16;
-        ccol[u] = (unsigned)(at < a.D - 16 ? at : a.D - 16);
+        ccol[u] = (unsigned)(at < a.Dc - 16 ? at : a.Dc - 16);
     }
 #pragma unroll
     for (int u = 0; u < Sh::UY; ++u) {
         const int q = wave * Sh::UY + u < Sh::YQ ? wave * Sh::UY + u : Sh::YQ - 1;
         yrow[u] = q * (64 / YL) + lane / YL;
         const int at = r0 * 2 + ((lane % YL) ^ (yswizzle(yrow[u]) << 1)) * 16;
-        ycol[u] = (unsigned)(at < a.R * 2 - 16 ? at : a.R * 2 - 16);
+        ycol[u] = (unsigned)(at < a.Rc * 2 - 16 ? at : a.Rc * 2 - 16);
     }
     const unsigned ldC = (unsigned)a.ldC, ldY = (unsigned)a.ldY * 2, ldS = (unsigned)a.ldS * 4;
     auto request = [&](int s, int slot) {
@@ -527,26 +530,59 @@ checkpoint_grad_ring_kernel(GradArgs a) {
         }
         wait_vmcnt<0>();                                   // no copy is under way when the workgroup gives its LDS back
     }
-    // a lane holds four columns of one row (D is a multiple of four)
+    // a lane holds four columns of one row
     if (gt + gl >= groups) return;
+    auto put = [&](auto *rows, auto tail) {                // rows of D columns
+        typedef std::remove_pointer_t<decltype(rows)> E;
 #pragma unroll
-    for (int n = 0; n < CN; ++n) {
-        const int r = r0 + n * 16 + l16;
-        if (r >= a.R) continue;
+        for (int n = 0; n < CN; ++n) {
+            const int r = r0 + n * 16 + l16;
+            if (r >= a.R) continue;
 #pragma unroll
-        for (int m = 0; m < CM; ++m) {
-            const int d = g * kGroup + c0 + m * 16 + quad * 4;
-            if (d >= a.D) continue;
-            if (!seg.whole) {
-                *(f32x4 *)(a.planes + (j * a.R + r) * (int64_t)a.D + d) = acc[m][n];
-            } else {
-                Out x[4];
+            for (int m = 0; m < CM; ++m) {
+                const int d = g * kGroup + c0 + m * 16 + quad * 4, left = a.D - d;
+                if (left <= 0) continue;
+                E x[4], *out = rows + (int64_t)r * a.D + d;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = sizeof(Out) == 2 ? (Out)bf16_bits(acc[m][n][i]) : (Out)acc[m][n][i];
-                __builtin_memcpy((Out *)a.G + seg.e * a.ldG + (int64_t)r * a.D + d, x, sizeof x);
+                for (int i = 0; i < 4; ++i) x[i] = sizeof(E) == 2 ? (E)bf16_bits(acc[m][n][i]) : (E)acc[m][n][i];
+                if (!tail || left >= 4) __builtin_memcpy(out, x, sizeof x);
+                else
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) if (i < left) out[i] = x[i];
             }
         }
-    }
+    };
+    auto put_all = [&](auto tail) {
+        if (seg.whole) put((Out *)a.G + seg.e * a.ldG, tail);
+        else put(a.planes + j * a.R * (int64_t)a.D, tail);
+    };
+    if (a.D % 4 == 0) put_all(std::false_type());          // (the code of partial stores is not fetched)
+    else put_all(std::true_type());
+}
+
+// Rows of `cols` elements copied to rows of ld (whole 16-byte chunks) with zeros behind them, a chunk a thread.
+template <class T>
+__global__ void __launch_bounds__(256)
+checkpoint_pack_kernel(const T *in, int64_t ld_in, int64_t rows, int32_t cols, T *out, int32_t ld) {
+    constexpr int E = 16 / sizeof(T);
+    const int chunks = ld / E;
+    const int64_t first = (int64_t)blockIdx.x * 256, r0 = first / chunks;
+    const unsigned at = (unsigned)(first - r0 * chunks) + threadIdx.x, up = at / (unsigned)chunks;
+    const int64_t r = r0 + up;
+    const int c = (int)(at - up * (unsigned)chunks) * E;
+    if (r >= rows) return;
+    T x[E];
+    const T *from = in + r * ld_in + c;
+    if (c + E <= cols) __builtin_memcpy(x, from, 16);
+    else
+#pragma unroll
+        for (int i = 0; i < E; ++i) x[i] = c + i < cols ? from[i] : (T)0;
+    __builtin_memcpy(__builtin_assume_aligned(out + r * ld + c, 16), x, 16);
+}
+template <class T>
+static void launch_pack(const T *in, int64_t ld_in, int64_t rows, int32_t cols, T *out, int32_t ld, hipStream_t st) {
+    const int64_t chunks = rows * (ld / (16 / (int)sizeof(T)));
+    hipLaunchKernelGGL(checkpoint_pack_kernel<T>, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, st, in, ld_in, rows, cols, out, ld);
 }
 
 // The planes of the examples of more than one segment, added in the order of their tokens.
@@ -633,22 +669,40 @@ static qless_status launch_many(const GradArgs &a, hipStream_t st) {
     uint16_t *x = (uint16_t *)a.planes;
     const int64_t ld = expand_ld(a.D), blocks = a.n + a.T / 64;
     if (blocks > 0x7FFFFFFF / (64 * TERMS)) return QLESS_ERR_UNSUPPORTED;
-    const ProductArgs p{ProductOperand{x, ld * 2, ld * 2, blocks * 64 * TERMS}, ProductOperand{a.dY, a.ldY * 2, (int64_t)a.R * 2, 0},
+    const ProductArgs p{ProductOperand{x, ld * 2, ld * 2, blocks * 64 * TERMS}, ProductOperand{a.dY, a.ldY * 2, (int64_t)a.Rc * 2, 0},
                         a.R, a.T, nullptr, nullptr, (a.D + 255) / 256, (int32_t)a.n, a.offsets};
     hipLaunchKernelGGL(checkpoint_expand_kernel<TERMS>, dim3((unsigned)blocks, (unsigned)((ld + 127) / 128)), dim3(256), 0, st, a, x, ld);
     const qless_status rc = launch_product<GradTile, ACROSS, ACROSS, GradStore<Out>, TERMS>(p, typename GradStore<Out>::Args{(Out *)a.G, a.ldG, a.R, a.D}, st);
     return rc == QLESS_OK ? launch_status() : rc;
 }
 
-// Tokens of a segment: one for each of the two workgroups of a compute unit, if all were full (the longest example would keep few of
-// them busy for long: rank 16, 64 ragged examples of 32768 tokens 64 us in segments of 2048, 48 of 512, 52 of 256), but none so short that its plane (written and read, 8 R bytes per column) costs more than its codes.
-static int64_t grad_chunk(int64_t T, int32_t R, int32_t D) {
-    const int64_t tiles = ((R + 127) / 128) * ((D + 4 * kGroup - 1) / (4 * kGroup)) * (R > 64 ? 2 : 1);
-    int64_t chunk = T * tiles / (2 * (int64_t)compute_units());
-    if (chunk < 8 * (int64_t)R) chunk = 8 * (int64_t)R;
+// Tokens of a segment.  32 tokens take a workgroup about half a microsecond, a plane the whole memory 8 R D bytes' time.  Where the
+// examples do not fill the two workgroups of each compute unit, they are cut into as many segments as do, or at which one more of
+// each would cost by its plane what it saves (1 x 8192 tokens, R = D = 1024 in one piece 262 us, in six 52, in twelve 58; 16 x 512,
+// R = 64, D = 4096 in whole examples 35, in four 42); where they do, into what each of those has to do if all were alike: the longest
+// example would keep few of them busy for long (rank 16, 64 ragged examples of 32768 tokens 64 us in segments of 2048, 48 of
+// 512, 52 of 256), but none so short that its plane costs more than its codes.
+static int64_t grad_chunk(int64_t T, int64_t n, int32_t R, int32_t D) {
+    const int64_t tiles = ((R + 127) / 128) * ((D + 4 * kGroup - 1) / (4 * kGroup)) * (R > 64 ? 2 : 1), slots = 2 * (int64_t)compute_units();
+    const int64_t mean = T / n + 1;
+    int64_t chunk;
+    if (n * tiles < slots) {
+        const double segments = fmin((double)slots / (double)(n * tiles), sqrt((double)mean * 0.8e5 / (8.0 * R * D * (double)n)));
+        chunk = segments < 0.5 ? 2 * mean : segments < 1.0 ? mean : (int64_t)((double)mean / segments) + 1;
+    } else {
+        chunk = T * tiles / slots;
+        if (chunk < 8 * (int64_t)R) chunk = 8 * (int64_t)R;
+    }
     if (chunk < 128) chunk = 128;
     if (chunk >= T) chunk = T + 1;
     return (chunk + 63) / 64 * 64;
+}
+static size_t up16(size_t bytes) { return (bytes + 15) & ~(size_t)15; }
+// Rows that are no whole chunks are packed into the workspace, whatever they lie in: gradients first, then codes.
+static int32_t packed_R(int32_t R) { return (R + 7) / 8 * 8; }
+static int32_t packed_D(int32_t D) { return (D + 15) / 16 * 16; }
+static size_t packed_bytes(int64_t T, int32_t R, int32_t D) {
+    return (R % 8 ? (size_t)T * packed_R(R) * 2 : 0) + (D % 16 ? (size_t)T * packed_D(D) : 0);
 }
 static int64_t grad_segments(int64_t T, int64_t n, int64_t chunk) { return n + T / chunk; }
 
@@ -741,9 +795,9 @@ extern "C" qless_status qless_checkpoint8_read(const int8_t *codes, int64_t ldC,
 extern "C" size_t qless_checkpoint8_grad_workspace(int64_t T, int64_t n, int32_t R, int32_t D) {
     using namespace qless;
     if (T < 0 || n < 1 || R < 1 || D < 1) return 0;
-    const int64_t segments = grad_segments(T, n, grad_chunk(T, R, D));
+    const int64_t segments = grad_segments(T, n, grad_chunk(T, n, R, D));
     const size_t planes = segments > n ? (size_t)segments * (size_t)R * (size_t)D * 4 : 0, rows = many_rows(T, n, R, D) ? expand_bytes(T, n, D, 2) : 0;
-    return planes > rows ? planes : rows;
+    return up16((planes > rows ? planes : rows)) + packed_bytes(T, R, D);
 }
 
 extern "C" qless_status qless_checkpoint8_grad(const void *dY, qless_dtype dtY, int64_t ldY, int32_t R, const int8_t *codes, int64_t ldC,
@@ -756,19 +810,33 @@ extern "C" qless_status qless_checkpoint8_grad(const void *dY, qless_dtype dtY, 
     if (n > 1 && ldG < (int64_t)R * D) return QLESS_ERR_INVALID_ARG;
     if (n == 0) return QLESS_OK;
     if (!offsets || !G || (T > 0 && (!dY || !codes || !step))) return QLESS_ERR_INVALID_ARG;
-    GradArgs a{dY, ldY, codes, ldC, step, ldS, offsets, n, T, grad_chunk(T, R, D), 0, R, D, 0, 0, G, ldG, (float *)ws};
+    GradArgs a{dY, ldY, codes, ldC, step, ldS, offsets, n, T, grad_chunk(T, n, R, D), 0, R, D, 0, 0, R, D, G, ldG, (float *)ws};
     a.segments = grad_segments(T, n, a.chunk);
     const size_t need = qless_checkpoint8_grad_workspace(T, n, R, D);
     if (need > 0 && (!ws || ws_bytes < need || ((uintptr_t)ws & 15) != 0)) return QLESS_ERR_WORKSPACE;
     const qless_status ready = device_ready();
     if (ready != QLESS_OK) return ready;
     const hipStream_t st = (hipStream_t)stream;
-    // 16-byte copies and 32-bit offsets
-    const bool whole_y = dtY == QLESS_BF16 && R % 8 == 0 && (T <= 1 || ldY % 8 == 0) && ((uintptr_t)dY & 15) == 0 && ldY < (1 << 22) && T <= 0x3FFFFFFF;
-    const bool whole = whole_y && D % 16 == 0 && (T <= 1 || ldC % 16 == 0) && ((uintptr_t)codes & 15) == 0 && ldC < (1 << 24) && ldS < (1 << 24);
-    if (whole_y && T > 1 && expand_ld(D) < (1 << 22) && many_rows(T, n, R, D))
-        return dtG == QLESS_BF16 ? launch_many<1, uint16_t>(a, st) : launch_many<2, float>(a, st);
-    if (whole) return dtG == QLESS_BF16 ? launch_ring_rows<uint16_t>(a, st) : launch_ring_rows<float>(a, st);
+    if (dtY == QLESS_BF16 && T > 0 && T <= 0x3FFFFFFF && (int64_t)T * (packed_R(R) / 8) < ((int64_t)1 << 38) && (int64_t)T * (packed_D(D) / 16) < ((int64_t)1 << 38)) {
+        unsigned char *pack = (unsigned char *)ws + (need - packed_bytes(T, R, D));
+        const bool many = expand_ld(D) < (1 << 22) && many_rows(T, n, R, D);
+        if (R % 8 != 0) {
+            a.Rc = packed_R(R);
+            launch_pack((const uint16_t *)dY, ldY, T, R, (uint16_t *)pack, a.Rc, st);
+            a.dY = pack; a.ldY = a.Rc;
+            pack += (size_t)T * a.Rc * 2;
+        }
+        if (D % 16 != 0 && !many) {
+            a.Dc = packed_D(D);
+            launch_pack(codes, ldC, T, D, (int8_t *)pack, a.Dc, st);
+            a.codes = (const int8_t *)pack; a.ldC = a.Dc;
+        }
+        // 16-byte copies and 32-bit offsets
+        const bool whole_y = (T == 1 || a.ldY % 8 == 0) && ((uintptr_t)a.dY & 15) == 0 && a.ldY < (1 << 22);
+        if (whole_y && many) return dtG == QLESS_BF16 ? launch_many<1, uint16_t>(a, st) : launch_many<2, float>(a, st);
+        if (whole_y && (T == 1 || a.ldC % 16 == 0) && ((uintptr_t)a.codes & 15) == 0 && a.ldC < (1 << 24) && ldS < (1 << 24))
+            return dtG == QLESS_BF16 ? launch_ring_rows<uint16_t>(a, st) : launch_ring_rows<float>(a, st);
+    }
     if (dtY == QLESS_BF16) return dtG == QLESS_BF16 ? launch_grad_rows<uint16_t, 2, uint16_t>(a, st) : launch_grad_rows<uint16_t, 2, float>(a, st);
     return dtG == QLESS_BF16 ? launch_grad_rows<float, 2, uint16_t>(a, st) : launch_grad_rows<float, 3, float>(a, st);
 }

@@ -146,7 +146,7 @@ WHOLE = [  # R in eights, D in sixteens: rows of whole chunks
 
 @pytest.mark.parametrize("dtY,dtG", [(torch.bfloat16, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.float32, torch.float32),
                                      (torch.float32, torch.bfloat16)])
-@pytest.mark.parametrize("R,D,ends,pad", [(*c, 1) for c in CASES] + [(*c, 0) for c in WHOLE])
+@pytest.mark.parametrize("R,D,ends,pad", [(*c, 1) for c in CASES] + [(*c, 0) for c in WHOLE] + [(*c, 1) for c in WHOLE[1:9]])
 def test_weight_gradients(R, D, ends, pad, dtY, dtG):
     _say("gradient R=%d D=%d ends=%s pad=%d %s %s" % (R, D, ends, pad, dtY, dtG))
     T = ends[-1] + 9                                  # tokens behind the last example
