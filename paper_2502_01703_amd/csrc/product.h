@@ -46,8 +46,10 @@ template <int KIND, int EXT, int NW> struct ProductCopies {
         ld = (int)op.ld;
         left_there = (int)op.depth % WHOLE;
         short_stage = left_there ? (int)op.depth / WHOLE : -1;
-        base = (const unsigned char *)op.base + (KIND == ALONG ? (int64_t)first * ld : (int64_t)first * 2);
-        const int64_t there = KIND == ALONG ? op.extent - 1 - first : op.extent - (int64_t)first * 2 - 16;     // of rows, or of a row's bytes
+        // (a tile that lies outside altogether reads the last row, or chunk)
+        const int64_t end = KIND == ALONG ? op.extent - 1 : op.extent / 2 - 8, at = first < end ? first : end;
+        base = (const unsigned char *)op.base + (KIND == ALONG ? at * ld : at * 2);
+        const int64_t there = KIND == ALONG ? end - at : (end - at) * 2;       // of rows, or of a row's bytes
         const int left = there < 65536 ? (int)there : 65536;   // more than a tile
 #pragma unroll
         for (int u = 0; u < U; ++u) {

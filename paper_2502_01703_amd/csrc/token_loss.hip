@@ -33,14 +33,16 @@ struct LossTokens {                        // workspace views, by live token (pa
     uint16_t *delta;                       // [Tp][piece]
     uint16_t *pack;                        // [piece][Dp] where W cannot be read as it lies
     float *planes;                         // [splits][Tp][Dp] partial dH
+    float *raw;                            // [raw][Tp][Vp] partial logits of small vocabularies
 };
 struct LossPlan {
     int64_t T, Tp, Dp, Vp, piece, parts;
-    int32_t D, V, tile_n, splits;
+    int32_t D, V, tile_n, tile_m, splits, raw;
     bool one_pass;                         // dW without a second pass
-    size_t off[18], total;
+    size_t off[19], total;
 };
 
+constexpr int kGather = 1024;              // entries of a part where partial logits are added
 constexpr int kFew = 32;                   // tokens up to which the rest of delta is two terms: rows t and t + kFew of delta and H
 
 constexpr int kLossThreads = 1024;
@@ -436,6 +438,42 @@ loss_delta_kernel(LossTokens w, int64_t Tp, int64_t parts, int64_t first, int64_
     }
 }
 
+// Partial logits added, with what the tiles' epilogue leaves of whole ones: a workgroup kGather entries of a token.
+template <bool STORE>
+__global__ void __launch_bounds__(256)
+loss_gather_kernel(LossTokens w, int64_t Tp, int64_t Vp, int raw, int32_t V) {
+    __shared__ float s_top[4], s_sum[4];
+    const int64_t t = blockIdx.x;
+    if (t >= *w.count) return;
+    const int c = (int)blockIdx.y * kGather + 4 * (int)threadIdx.x;
+    f32x4 z = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    if (c < Vp) {
+        z = *(const f32x4 *)(w.raw + t * Vp + c);
+#pragma unroll 4
+        for (int s = 1; s < raw; ++s) z += *(const f32x4 *)(w.raw + (s * Tp + t) * Vp + c);
+        const int y = w.target[t] - c;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (u == y) w.hit[t] = z[u];
+            if (c + u >= V) z[u] = -INFINITY;
+        }
+        if (STORE) *(f32x4 *)(w.logits + t * Vp + c) = z;
+    }
+    float top = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]));
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
+    if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+    const float ref = top == -INFINITY ? 0.0f : top;
+    float sum = (__expf(z[0] - ref) + __expf(z[1] - ref)) + (__expf(z[2] - ref) + __expf(z[3] - ref));
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) sum += __shfl_xor(sum, d, 64);
+    if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) w.part[(int64_t)blockIdx.y * Tp + t] = make_float2(top, (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]));
+}
+
 // The live tokens in the order of target and token, and where each 64 vocabulary entries begin there: 16 threads count what comes before
 // a token (or before 64 entries).  T (T + V / 64) comparisons, next to the 2 T D V operations of the products.
 __global__ void __launch_bounds__(256)
@@ -530,9 +568,11 @@ loss_hidden_kernel(LossTokens w, int64_t Tp, int64_t Dp, int32_t D, int splits, 
 }
 
 typedef ProductShape<256, 256, 2, 4, 2> Loss256;
+typedef ProductShape<128, 256, 2, 4, 3> LossHalf;
 typedef ProductShape<256, 128, 4, 2, 3> Loss128;
 typedef ProductShape<256, 64, 8, 1, 4> Loss64;
 typedef ProductShape<256, 32, 8, 1, 4> Loss32;
+typedef ProductShape<128, 128, 2, 2, 2> LossSmall;         // dW where larger tiles do not fill the chip
 
 static int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
@@ -544,14 +584,28 @@ static LossPlan loss_plan(int64_t T, int32_t D, int32_t V, bool want_dH, bool wa
     p.Tp = up_to(T > 0 ? T : 1, p.tile_n < 64 ? 64 : p.tile_n);
     p.Dp = up_to(D, 64);
     p.Vp = up_to(V, 256);
-    p.parts = p.Vp / 32;                                    // at most (32 entries a part)
-    if (p.tile_n == 256) p.parts = p.Vp / 128;
-    if (p.tile_n == 128) p.parts = p.Vp / 64;
     const bool gradient = want_dH || want_dW;
     // A piece: logits and delta of up to 1.5 GB.  (Their 10 bytes a logit come from memory at any size that is worth its additions to
     // the planes, and more tiles fill their last round better.)  With dW one piece saves the second pass.  Few tokens: one piece.
     const int64_t budget = (int64_t)1536 << 20, cus = compute_units();
     const int64_t ntiles = (T + p.tile_n - 1) / p.tile_n;
+    // The tiles of logits where few fill the chip: rounds of tiles of 128 entries, at 0.64 of the larger ones' time each (256 x 4096 x 32000,
+    // loss alone: 102 -> 79 us), or D in parts, whose partial logits another kernel adds in 8 us and their bytes' time (256 x 8192 x 4000: 157 -> 52 us).  A
+    // stage of 64 columns takes 1.6 us in a tile of 256 tokens; with few tokens 0.5, and half of the chip reads W as fast as all
+    // of it (1 x 4096 x 32000 in two parts 49 -> 53 us).
+    const int64_t tiles_m = p.Vp / 256 * (ntiles > 0 ? ntiles : 1);
+    const double rounds = (double)((tiles_m + cus - 1) / cus), half_rounds = 0.64 * (double)((2 * tiles_m + cus - 1) / cus);
+    const bool halves = p.tile_n == 256 && half_rounds < rounds, narrow = p.tile_n <= 64;
+    p.tile_m = halves ? 128 : 256;
+    p.raw = 1;
+    int64_t raw = cus / tiles_m > 0 ? cus / tiles_m : 1;
+    if (raw > p.Dp / 64 / 4) raw = p.Dp / 64 / 4 > 0 ? p.Dp / 64 / 4 : 1;
+    const double saved = (double)(p.Dp / 64) * (narrow ? 0.5 : p.tile_n == 128 ? 0.8 : 1.6) * ((halves ? 0.64 : 1.0) - 1.0 / (double)raw);
+    if (raw >= (narrow ? 3 : 2) && saved > 8.0 + (double)T * (double)p.Vp * 8.0 * (double)raw / 5e6) {
+        p.raw = (int32_t)raw;
+        p.tile_m = 256;
+    }
+    p.parts = p.Vp / 32;                                    // at most (32 entries a part)
     p.one_pass = T <= kFew || p.Tp * p.Vp * 6 <= budget;
     int64_t piece = p.Vp;
     if (!p.one_pass) {
@@ -585,6 +639,7 @@ static LossPlan loss_plan(int64_t T, int32_t D, int32_t V, bool want_dH, bool wa
     if (packed < each * 256) packed = each * 256;
     take(whole > packed ? whole : packed);
     take(want_dH ? (size_t)p.splits * p.Tp * p.Dp * 4 : 0); // 16 planes
+    take(p.raw > 1 ? (size_t)p.raw * p.Tp * p.Vp * 4 : 0);  // 17 raw
     p.total = at;
     return p;
 }
@@ -597,6 +652,13 @@ static qless_status loss_product(int tile_n, const ProductArgs &a, const typenam
         case 128: return launch_product<Loss128, AK, BK, Epilogue>(a, e, st);
         default: return launch_product<Loss256, AK, BK, Epilogue>(a, e, st);
     }
+}
+// the tiles of logits of `entries` from the vocabulary
+template <class Epilogue>
+static qless_status logits_product(const LossPlan &p, ProductArgs a, int64_t entries, const typename Epilogue::Args &e, hipStream_t st) {
+    a.mtiles = (int32_t)((entries + p.tile_m - 1) / p.tile_m);
+    if (p.tile_m == 128) return launch_product<LossHalf, ALONG, ALONG, Epilogue>(a, e, st);
+    return loss_product<Epilogue, ALONG, ALONG>(p.tile_n, a, e, st);
 }
 
 }  // namespace qless
@@ -628,7 +690,7 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
     w.token = ints(2); w.target = ints(3); w.place = ints(4);
     w.weight = floats(5); w.lse = floats(6); w.hit = floats(7); w.top = floats(8); w.sum = floats(9); w.shrink = floats(10); w.pull = floats(11);
     w.part = (float2 *)(base + p.off[12]); w.order = ints(13); w.order_target = w.order + p.Tp; w.start = ints(14);
-    w.logits = floats(15); w.planes = floats(16);
+    w.logits = floats(15); w.planes = floats(16); w.raw = floats(17);
 
     // W is read where it lies if its rows are whole 16-byte chunks; else a piece at a time is packed into the workspace
     const bool packs = ((uintptr_t)W & 15) != 0 || (ldW % 8 != 0 && V > 1) || D % 8 != 0 || ldW * 2 >= ((int64_t)1 << 23);
@@ -658,7 +720,12 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
     auto head_product = [&](int64_t n, int64_t v0) {        // dW: rows m columns of H, columns n entries
         ProductArgs a{ProductOperand{w.H, p.Dp * 2, p.Dp * 2, p.Tp}, ProductOperand{w.delta, piece * 2, up_to(n, 64) * 2, few ? 2 * kFew : p.Tp},
                       n, T == 0 ? 0 : few ? 2 * kFew : p.Tp, nullptr, few ? nullptr : w.count, (D + 255) / 256, 1};
-        return launch_product<Loss256, ACROSS, ACROSS, LossHead>(a, LossHead::Args{(uint16_t *)dW, ldDW, v0, V, D, w.order, w.order_target, w.start, w.pull, w.H, p.Dp}, st);
+        const LossHead::Args e{(uint16_t *)dW, ldDW, v0, V, D, w.order, w.order_target, w.start, w.pull, w.H, p.Dp};
+        if (a.mtiles * ((n + 255) / 256) < compute_units()) {            // 512 x 512 x 2000: 104 -> 86 us; a chip full of the larger ones is 5 % faster
+            a.mtiles = (D + 127) / 128;
+            return launch_product<LossSmall, ACROSS, ACROSS, LossHead>(a, e, st);
+        }
+        return launch_product<Loss256, ACROSS, ACROSS, LossHead>(a, e, st);
     };
 
     if (T <= 64) {
@@ -670,25 +737,35 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
     if (dW)
         hipLaunchKernelGGL(loss_order_kernel, dim3((unsigned)((T + 15) / 16 + (p.Vp / 64 + 1 + 15) / 16)), dim3(256), 0, st, w, T, p.Vp / 64 + 1);
     qless_status rc = QLESS_OK;
-    const int per_part = p.tile_n == 256 ? 128 : p.tile_n == 128 ? 64 : 32;
+    const bool raw = p.raw > 1 && piece == p.Vp;
+    const int per_part = raw ? kGather : p.tile_m == 128 ? 64 : p.tile_n == 256 ? 128 : p.tile_n == 128 ? 64 : 32;
+    auto parts_of = [&](int64_t entries) { return (entries + per_part - 1) / per_part; };
 
     // first pass: the losses, and dH unless delta comes with dW
     const bool run = dH && (!one_pass || (!dW && T >= 256));    // (fewer tokens: their rows are shared out, which takes lse first)
+    const bool store = dH || one_pass;
     for (int64_t v0 = 0; T > 0 && v0 < V && rc == QLESS_OK; v0 += piece) {
         const int64_t n = rows_of(v0), np = up_to(n, 256);
         const ProductOperand rows = head(v0);
-        const ProductArgs a{rows, tokens, T, p.Dp, w.count, nullptr, (int32_t)(np / 256), 1};
-        if (!dH && !one_pass) {
-            rc = loss_product<LossStats<false, true>, ALONG, ALONG>(p.tile_n, a, LossStats<false, true>::Args{w.target, w.hit, w.part, p.Tp, v0, V, nullptr, 0}, st);
-            continue;
+        const ProductArgs a{rows, tokens, T, p.Dp, w.count, nullptr, 0, raw ? p.raw : 1, nullptr};
+        if (raw) {
+            rc = logits_product<LossPlane<false>>(p, a, np, LossPlane<false>::Args{w.raw, p.Tp, p.Vp, nullptr}, st);
+            const dim3 grid((unsigned)T, (unsigned)parts_of(p.Vp));
+            if (store) hipLaunchKernelGGL(loss_gather_kernel<true>, grid, dim3(256), 0, st, w, p.Tp, p.Vp, p.raw, V);
+            else hipLaunchKernelGGL(loss_gather_kernel<false>, grid, dim3(256), 0, st, w, p.Tp, p.Vp, p.raw, V);
+        } else if (!store) {
+            rc = logits_product<LossStats<false, true>>(p, a, np, LossStats<false, true>::Args{w.target, w.hit, w.part, p.Tp, v0, V, nullptr, 0}, st);
+        } else if (run) {
+            rc = logits_product<LossStats<true, false>>(p, a, np, LossStats<true, false>::Args{w.target, w.hit, w.part, p.Tp, v0, V, w.logits, piece}, st);
+        } else {
+            rc = logits_product<LossStats<true, true>>(p, a, np, LossStats<true, true>::Args{w.target, w.hit, w.part, p.Tp, v0, V, w.logits, piece}, st);
         }
-        if (run) rc = loss_product<LossStats<true, false>, ALONG, ALONG>(p.tile_n, a, LossStats<true, false>::Args{w.target, w.hit, w.part, p.Tp, v0, V, w.logits, piece}, st);
-        else rc = loss_product<LossStats<true, true>, ALONG, ALONG>(p.tile_n, a, LossStats<true, true>::Args{w.target, w.hit, w.part, p.Tp, v0, V, w.logits, piece}, st);
+        if (!store) continue;
         if (rc != QLESS_OK) break;
         int64_t shares = run || T >= 1024 ? 1 : 1024 / T + 1;                  // of a row
         if (shares > np / 1024) shares = np / 1024 > 0 ? np / 1024 : 1;
         const dim3 grid((unsigned)up_to(T, few ? kFew : 64), (unsigned)shares);
-        const int64_t parts = np / per_part;
+        const int64_t parts = parts_of(np);
         auto delta = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, w, p.Tp, parts, v0, np, piece, nll, lse); };
         if (run) few ? delta(loss_delta_kernel<true, true>) : delta(loss_delta_kernel<true, false>);
         else few ? delta(loss_delta_kernel<false, true>) : delta(loss_delta_kernel<false, false>);
@@ -696,8 +773,8 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
         if (rc == QLESS_OK && dW && one_pass) rc = head_product(n, v0);
     }
     if (rc != QLESS_OK) return rc;
-    if (T > 0 && !dH && !one_pass) {
-        const int64_t parts = p.Vp / per_part;
+    if (T > 0 && !store) {
+        const int64_t parts = parts_of(p.Vp);
         if (T <= 64) hipLaunchKernelGGL(loss_join_kernel<1>, dim3((unsigned)T), dim3(256), 0, st, w, p.Tp, parts, nll, lse);
         else hipLaunchKernelGGL(loss_join_kernel<4>, dim3((unsigned)((T + 3) / 4)), dim3(256), 0, st, w, p.Tp, parts, nll, lse);
     }
@@ -715,7 +792,7 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
     // second pass: delta from the known losses, a piece at a time, and dW
     for (int64_t v0 = 0; dW && (!one_pass || T == 0) && v0 < V && rc == QLESS_OK; v0 += piece) {
         const int64_t n = rows_of(v0);
-        const ProductArgs a{head(v0), tokens, T, p.Dp, w.count, nullptr, (int32_t)(up_to(n, 256) / 256), 1};
+        const ProductArgs a{head(v0), tokens, T, p.Dp, w.count, nullptr, (int32_t)(up_to(n, 256) / 256), 1, nullptr};
         if (few) rc = launch_product<Loss32, ALONG, ALONG, LossDelta<true>>(a, LossDelta<true>::Args{w.target, w.lse, w.weight, w.delta, piece, v0, V}, st);
         else rc = loss_product<LossDelta<false>, ALONG, ALONG>(p.tile_n, a, LossDelta<false>::Args{w.target, w.lse, w.weight, w.delta, piece, v0, V}, st);
         if (rc == QLESS_OK) rc = head_product(n, v0);

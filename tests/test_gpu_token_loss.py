@@ -75,7 +75,7 @@ def _check(H, W, y, w, got):
 
 
 SIZES = [(1, 1, 1), (1, 64, 2), (1, 8, 1000), (2, 72, 257), (1, 4096, 300), (31, 100, 256), (32, 128, 2049), (33, 520, 255), (257, 129, 1000), (300, 64, 513),
-         (300, 264, 3001), (513, 8, 700), (64, 1000, 5000)]
+         (300, 264, 3001), (513, 8, 700), (64, 1000, 5000), (200, 4104, 700), (513, 2056, 1000), (700, 72, 100), (150, 640, 9000)]
 
 
 @pytest.mark.parametrize("T,D,V", SIZES)
