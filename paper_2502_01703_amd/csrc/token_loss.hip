@@ -16,6 +16,7 @@
 // wrong.)  Up to 32 tokens, where the products wait for W anyway, the rest goes in as the sum of two bfloat16 numbers.
 #include "product.h"
 #include "score.h"
+#include "token_loss.h"
 
 namespace qless {
 
@@ -291,16 +292,6 @@ struct LossHead {
         });
     }
 };
-
-// Maximum and sum (relative to it) of one token over parts p, p + lanes, ..; then of two such pairs.
-__device__ inline void join_pair(float &top, float &sum, float top2, float sum2) {
-    const float next = fmaxf(top, top2);
-    if (next == -INFINITY) sum += sum2;                     // 0, or NaN of logits that are not numbers
-    else sum = sum * __expf(top - next) + sum2 * __expf(top2 - next);
-    top = next;
-}
-// near 0 the loss keeps its digits
-__device__ inline float loss_of(float top, float sum, float hit) { return logf(sum) + (top - hit); }
 
 // lse and nll of TOK tokens from their parts, 256 / TOK threads each.
 template <int TOK>
@@ -666,7 +657,8 @@ static qless_status logits_product(const LossPlan &p, ProductArgs a, int64_t ent
 extern "C" size_t qless_token_loss_workspace(int64_t T, int32_t D, int32_t V, int want_dH, int want_dW) {
     using namespace qless;
     if (T < 0 || D < 1 || V < 1) return 0;
-    return loss_plan(T, D, V, want_dH != 0, want_dW != 0).total;
+    const size_t total = loss_plan(T, D, V, want_dH != 0, want_dW != 0).total, single = want_dH && !want_dW ? single_workspace(T, D, V) : 0;
+    return total > single ? total : single;
 }
 
 extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void *W, int64_t ldW, qless_dtype dt, int64_t T, int32_t D, int32_t V,
@@ -677,11 +669,15 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
     if (dt != QLESS_BF16 || D > 65536 || T > 0x3FFFFFFF) return QLESS_ERR_UNSUPPORTED;
     if (T == 0 && !dW) return QLESS_OK;
     if (!W || (T > 0 && (!H || !target || !nll))) return QLESS_ERR_INVALID_ARG;
-    const LossPlan p = loss_plan(T, D, V, dH != nullptr, dW != nullptr);
-    if (!ws || ws_bytes < p.total || ((uintptr_t)ws & 15) != 0) return QLESS_ERR_WORKSPACE;
+    if (!ws || ws_bytes < qless_token_loss_workspace(T, D, V, dH != nullptr, dW != nullptr) || ((uintptr_t)ws & 15) != 0) return QLESS_ERR_WORKSPACE;
     const qless_status ready = device_ready();
     if (ready != QLESS_OK) return ready;
     const hipStream_t st = (hipStream_t)stream;
+    // W is read where it lies if its rows are whole 16-byte chunks; else a piece at a time is packed into the workspace
+    const bool packs = ((uintptr_t)W & 15) != 0 || (ldW % 8 != 0 && V > 1) || D % 8 != 0 || ldW * 2 >= ((int64_t)1 << 23);
+    if (dH && !dW && !packs && single_serves(T, D, V))
+        return launch_single((const uint16_t *)H, ldH, (const uint16_t *)W, V > 1 ? ldW : D, (int)T, D, V, target, weight, nll, lse, (uint16_t *)dH, ldDH, ws, st);
+    const LossPlan p = loss_plan(T, D, V, dH != nullptr, dW != nullptr);
     unsigned char *base = (unsigned char *)ws;
     auto ints = [&](int i) { return (int32_t *)(base + p.off[i]); };
     auto floats = [&](int i) { return (float *)(base + p.off[i]); };
@@ -692,8 +688,6 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
     w.part = (float2 *)(base + p.off[12]); w.order = ints(13); w.order_target = w.order + p.Tp; w.start = ints(14);
     w.logits = floats(15); w.planes = floats(16); w.raw = floats(17);
 
-    // W is read where it lies if its rows are whole 16-byte chunks; else a piece at a time is packed into the workspace
-    const bool packs = ((uintptr_t)W & 15) != 0 || (ldW % 8 != 0 && V > 1) || D % 8 != 0 || ldW * 2 >= ((int64_t)1 << 23);
     const bool gradient = dH || dW, few = T <= kFew;
     int64_t piece = gradient ? p.piece : p.Vp;
     if (packs) {

@@ -101,6 +101,37 @@ def test_loss_and_gradients(T, D, V, pads):
     _check(H, W, y, None, Q.token_loss(h, W_, y))
 
 
+@pytest.mark.parametrize("T,D,V", [(1, 8, 1), (1, 64, 7), (1, 2048, 5000), (1, 2056, 3001), (1, 4104, 1500), (1, 8192, 4097), (1, 8200, 600), (2, 200, 4000),
+                                   (2, 4096, 2500), (2, 8192, 1025), (3, 1000, 9000), (4, 2048, 2049), (4, 4096, 1000), (4, 4104, 800), (4, 16, 200000)])
+@pytest.mark.parametrize("pads", [(0, 0), (3, 8)])
+def test_up_to_four_tokens(T, D, V, pads):
+    _say("loss of few T=%d D=%d V=%d pads=%s" % (T, D, V, pads))
+    H, W, y, w = _inputs(T, D, V, T + D + V, masked=0.0)
+    h, _ = _inside(H, pads[0], 0)
+    W_, _ = _inside(W, pads[1], 0)
+    dH, wide = _inside(torch.zeros_like(H), pads[0], 2)
+    ws = torch.full((Q.token_loss_workspace(T, D, V),), 0xFF, dtype=torch.uint8, device=DEV)
+    got = Q.token_loss(h, W_, y, w, dH=dH, ws=ws)
+    _check(H, W, y, w, got)
+    assert (wide[:, :pads[0]] == 7).all() and (wide[:, pads[0] + D:] == 7).all()
+    for t in range(T):                                # each left out once, its row not a number
+        z = y.clone()
+        z[t] = (-100, V, 1 << 40, -1)[t]
+        g = H.clone()
+        g[t] = float("nan")
+        _check(H, W, z, None, Q.token_loss(g, W_, z))
+    for v in (0, V - 1):                              # targets at the ends
+        _check(H, W, torch.full_like(y, v), w, Q.token_loss(h, W_, torch.full_like(y, v), w))
+    if T > 1:
+        g = H.clone()
+        g[1, 0] = float("inf")
+        spoiled = Q.token_loss(g, W_, y, w)
+        good = torch.arange(T, device=DEV) != 1
+        for a, b in zip(got[:3], spoiled[:3]):
+            assert torch.equal(a[good], b[good])
+        assert not spoiled[0][1].isfinite() and not spoiled[2][1].isfinite().any()
+
+
 @pytest.mark.parametrize("T,D,V", [(9000, 40, 30000), (8192, 64, 20000), (1, 4100, 20000), (30, 4100, 20000), (2000, 72, 70000), (700, 100, 150000)])
 def test_pieces_of_the_vocabulary(T, D, V):
     """More vocabulary than a piece holds, read in place and packed."""
