@@ -366,15 +366,17 @@ checkpoint_grad_kernel(GradArgs a) {
 // The same for bfloat16 gradients and operands whose rows are whole 16-byte chunks (or were made so).  A workgroup takes RT rows of R x GROUPS groups, a
 // wavefront of it one group (or half of one); stages of 32 tokens' codes, gradients and steps are copied to a ring of NS in LDS
 // without passing through registers, three of them on their way while one is used: codes stay 8 bits wide until the transposing
-// reads have brought eight tokens of a column into a lane, and the step is multiplied there, into the gradients or, from 128 rows on,
+// reads have brought eight tokens of a column into a lane, and the step is multiplied there, into the gradients or, from 33 rows on,
 // into the codes (either product has 16 bits: two bfloat16 numbers).  Bound: memory while R is a rank of adapters (codes are read once
-// for 128 rows); the vector work of a stage is 12 operations for eight numbers of one side and 40 for eight of the other.
+// for 128 rows); the vector work of a stage is 12 operations for eight numbers of one side and 40 for eight of the other.  64 x 512 tokens
+// of 4096 columns: 47 us at R = 16, 37 of them the copies and their start; R = 64: 78 us in halves of a group per wavefront
+// with the steps in the codes, 98 in whole groups with the steps in the gradients (and half the wavefronts' room in registers).
 // Rows of 128 codes are exchanged by 16-byte chunks, rows of gradients by 32-byte pieces, so that the eight (four) rows of each of two
 // lane groups lie in different banks.
 template <int RT> struct GradRing {
-    static constexpr int NW = 4, SPLIT = RT >= 128 ? 2 : 1, GROUPS = NW / SPLIT, KT = 32, NS = 4, CM = 8 / SPLIT, CN = RT / 16;     // SPLIT: wavefronts of a group
+    static constexpr int NW = 4, SPLIT = RT >= 32 ? 2 : 1, GROUPS = NW / SPLIT, KT = 32, NS = 4, CM = 8 / SPLIT, CN = RT / 16;     // SPLIT: wavefronts of a group
     static constexpr int CODES = GROUPS * KT * 128, Y = KT * RT * 2, STAGE = CODES + Y + NW * 256, LDS = NS * STAGE;
-    static constexpr bool SCALE_CODES = RT >= 128;         // the side with fewer fragments takes the steps
+    static constexpr bool SCALE_CODES = RT >= 64;          // the side with fewer fragments takes the steps
     static constexpr int UC = 4 / SPLIT, YQ = Y / 1024, UY = (YQ + NW - 1) / NW, U = UC + UY + 1;
     static_assert((NS - 2) * U < 64, "vmcnt is a 6-bit counter");
 };
@@ -683,7 +685,7 @@ static qless_status launch_many(const GradArgs &a, hipStream_t st) {
 // example would keep few of them busy for long (rank 16, 64 ragged examples of 32768 tokens 64 us in segments of 2048, 48 of
 // 512, 52 of 256), but none so short that its plane costs more than its codes.
 static int64_t grad_chunk(int64_t T, int64_t n, int32_t R, int32_t D) {
-    const int64_t tiles = ((R + 127) / 128) * ((D + 4 * kGroup - 1) / (4 * kGroup)) * (R > 64 ? 2 : 1), slots = 2 * (int64_t)compute_units();
+    const int64_t tiles = ((R + 127) / 128) * ((D + 4 * kGroup - 1) / (4 * kGroup)) * (R > 16 ? 2 : 1), slots = 2 * (int64_t)compute_units();
     const int64_t mean = T / n + 1;
     int64_t chunk;
     if (n * tiles < slots) {
