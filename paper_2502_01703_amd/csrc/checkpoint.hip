@@ -380,10 +380,6 @@ template <int RT> struct GradRing {
     static constexpr int UC = 4 / SPLIT, YQ = Y / 1024, UY = (YQ + NW - 1) / NW, U = UC + UY + 1;
     static_assert((NS - 2) * U < 64, "vmcnt is a 6-bit counter");
 };
-__device__ inline void global_to_lds4(const void *base, unsigned lane_off, unsigned lds_addr) {      // lane L: LDS bytes [lds_addr + 4 L, + 4)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" :: "s"(lds_addr), "v"(lane_off), "s"(base) : "memory");
-}
-
 __device__ inline bf16x8 upper_halves(const float (&v)[8]) {
     union { uint32_t u[4]; bf16x8 b; } r;
 #pragma unroll
@@ -672,7 +668,7 @@ static qless_status launch_many(const GradArgs &a, hipStream_t st) {
     const int64_t ld = expand_ld(a.D), blocks = a.n + a.T / 64;
     if (blocks > 0x7FFFFFFF / (64 * TERMS)) return QLESS_ERR_UNSUPPORTED;
     const ProductArgs p{ProductOperand{x, ld * 2, ld * 2, blocks * 64 * TERMS}, ProductOperand{a.dY, a.ldY * 2, (int64_t)a.Rc * 2, 0},
-                        a.R, a.T, nullptr, nullptr, (a.D + 255) / 256, (int32_t)a.n, a.offsets};
+                        a.R, a.T, nullptr, nullptr, (a.D + 255) / 256, (int32_t)a.n, a.offsets, nullptr, 0, 0};
     hipLaunchKernelGGL(checkpoint_expand_kernel<TERMS>, dim3((unsigned)blocks, (unsigned)((ld + 127) / 128)), dim3(256), 0, st, a, x, ld);
     const qless_status rc = launch_product<GradTile, ACROSS, ACROSS, GradStore<Out>, TERMS>(p, typename GradStore<Out>::Args{(Out *)a.G, a.ldG, a.R, a.D}, st);
     return rc == QLESS_OK ? launch_status() : rc;

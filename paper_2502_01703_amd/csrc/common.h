@@ -69,6 +69,11 @@ __device__ inline void global_to_lds16(const void *base, unsigned lane_off, unsi
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                  :: "s"(lds_addr), "v"(lane_off), "s"(base) : "memory");
 }
+// Four bytes a lane: lane L writes LDS bytes [lds_addr + 4 L, + 4).
+__device__ inline void global_to_lds4(const void *base, unsigned lane_off, unsigned lds_addr) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+                 :: "s"(lds_addr), "v"(lane_off), "s"(base) : "memory");
+}
 template <int N> __device__ inline void wait_vmcnt() {
     static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit counter");
     asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory");

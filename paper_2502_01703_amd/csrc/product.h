@@ -34,6 +34,10 @@ struct ProductArgs {
     // CUTS: part e of K is the rows [cuts[e], cuts[e + 1]) of b (device; clamped to 0 .. k), its stages in a begin at stage
     // TERMS (e + cuts[e] / 64): each 64 rows of b meet TERMS stages of a, one after another, which are zeros behind the part's rows.
     const int64_t *cuts;
+    // SHIFT: b holds numbers that are not negative, and b(n, k) is to be multiplied by a power of two for each n and each 64 << shift_stages
+    // steps of K: shift[k / (64 << shift_stages)][n] takes it off the exponents of two such numbers at once (bits 7 on of each half), down
+    // to 0.  n up to whole tiles is read.
+    const uint32_t *shift; int64_t shift_ld; int32_t shift_stages;
 };
 
 template <int KIND, int EXT, int NW> struct ProductCopies {
@@ -112,6 +116,18 @@ template <int MT_, int NT_, int WY_, int WX_, int NS_> struct ProductShape {
     static_assert(FM * WY * 32 == MT && FN * WX * 32 == NT && NS >= 2 && NW * FM * 4096 <= LDS, "whole fragments, and room for 32 rows of them");
 };
 
+// Eight bfloat16 numbers that are not negative, each divided by the same power of two, to 0 if it is too great: a saturating subtraction
+// in the exponent field of two at a time.
+__device__ inline bf16x8 lower_exponents(bf16x8 x, uint32_t by) {
+    typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+    union { bf16x8 v; u16x2 u[4]; } r;
+    r.v = x;
+    const u16x2 b = __builtin_bit_cast(u16x2, by);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.u[i] = __builtin_elementwise_sub_sat(r.u[i], b);
+    return r.v;
+}
+
 // A wavefront's accumulators row by row of n: store(r, c, x) is called for every row r < 32 FN with four columns from c = 4 (lane % (8 FM))
 // on, so that lanes next to each other hold columns next to each other.  32 rows at a time pass through the wavefront's part of `lds`
 // (4 KB per FM), their 16-byte chunks exchanged by the row: the accumulators' own order, 16 to 32 bytes of 32 rows each, took the caches
@@ -146,7 +162,7 @@ __device__ inline void by_rows(unsigned char *lds, f32x16 (&acc)[FM][FN], Store 
 
 // Epilogue::run(args, lds, acc, m, n, split, live): acc[i][j][v] is C at m + 32 i + 8 (v / 4) + 4 half + v % 4, n + 32 j + lane % 32; lds: the
 // workgroup's, free.
-template <class Sh, int AK, int BK, class Epilogue, int CUTS = 0>
+template <class Sh, int AK, int BK, class Epilogue, int CUTS = 0, bool SHIFT = false>
 __global__ void __launch_bounds__(64 * Sh::NW, Sh::NW / 4)
 product_kernel(ProductArgs p, typename Epilogue::Args e) {
     constexpr int TERMS = CUTS ? CUTS : 1;
@@ -183,12 +199,15 @@ product_kernel(ProductArgs p, typename Epilogue::Args e) {
     constexpr int UA = ProductCopies<AK, Sh::MT, NW>::U, UB = ProductCopies<BK, Sh::NT, NW>::U;
     ca.init(p.a, m0, lane, wave);
     cb.init(p.b, n0, lane, wave);
-    constexpr int U = UA + UB;
+    constexpr int U = UA + UB + (SHIFT ? 1 : 0);
+    const int ma = wy * FM * 32, nb = wx * FN * 32;
     auto request = [&](int u, int s, int slot) {           // copy u of a stage; past the end the last one again: all stages count alike
         if (s > s1 - 1) s = s1 - 1;
         const unsigned at = lds0 + (unsigned)(slot * Sh::STAGE);
         if (u < UA) ca.issue(u, s, lane, wave, at);
-        else cb.issue(u - UA, s / TERMS, lane, wave, at + Sh::MT * 128);
+        else if (u < UA + UB) cb.issue(u - UA, s / TERMS, lane, wave, at + Sh::MT * 128);
+        else                                               // this wavefront's columns' shifts
+            global_to_lds4(p.shift + (int64_t)(s >> p.shift_stages) * p.shift_ld + n0 + nb, (unsigned)((lane & (32 * FN - 1)) * 4), lds0 + (unsigned)(NS * Sh::STAGE + (slot * NW + wave) * 256));
     };
     f32x16 acc[FM][FN];
 #pragma unroll
@@ -198,9 +217,14 @@ product_kernel(ProductArgs p, typename Epilogue::Args e) {
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
     const unsigned la = fragment_lane<AK, Sh::MT>(lane), lb = fragment_lane<BK, Sh::NT>(lane);
-    const int ma = wy * FM * 32, nb = wx * FN * 32;
     if (s0 < s1) {
+        static_assert(!SHIFT || FN <= 2, "a lane a column");
         bf16x8 fa[2][FM], fb[2][FN];
+        uint32_t by[2][FN];                                // shifts of the stage, and of the next
+        auto read_shift = [&](int set, int slot) {
+#pragma unroll
+            for (int j = 0; j < FN; ++j) by[set][j] = *(const uint32_t *)(smem + NS * Sh::STAGE + (slot * NW + wave) * 256 + (32 * j + (lane & 31)) * 4);
+        };
         auto read = [&](int set, int f, int slot, int kk) {          // fragment f of a K step of 16: the columns', then the rows'
             const unsigned char *sa = smem + slot * Sh::STAGE;
             if (f < FN) fb[set][f] = fragment<BK, Sh::NT>(sa + Sh::MT * 128, lb, nb + 32 * f, kk);
@@ -216,6 +240,7 @@ product_kernel(ProductArgs p, typename Epilogue::Args e) {
         asm volatile("" ::: "memory");
 #pragma unroll
         for (int f = 0; f < FM + FN; ++f) read(0, f, 0, 0);
+        if (SHIFT) read_shift(0, 0);
         int slot = 0;
         // The fragments of a K step are read while the products of the one before run.  The barrier of a stage stands behind the first
         // products of its last K step: by then every fragment of it is in registers, so the slot is free for the stage NS further on, and
@@ -227,6 +252,9 @@ product_kernel(ProductArgs p, typename Epilogue::Args e) {
                 constexpr int I = FM * FN, R = FM + FN, K0 = I > 2 ? 1 : 0;
                 const int cur = kk & 1;
                 const bool last = kk == 3;
+                if (SHIFT)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) fb[cur][j] = lower_exponents(fb[cur][j], by[0][j]);
 #pragma unroll
                 for (int i = 0; i < I; ++i) {
                     pin();
@@ -243,12 +271,16 @@ product_kernel(ProductArgs p, typename Epilogue::Args e) {
 #pragma unroll
                     for (int f = 0; f < R; ++f)
                         if (f * (I - first) / R + first == i) read(cur ^ 1, f, last ? next : slot, (kk + 1) & 3);
+                    if (SHIFT && last && i == I - 1) read_shift(1, next);
                     if (last)
 #pragma unroll
                         for (int u = 0; u < U; ++u)
                             if (u * (I - first) / U + first == i) request(u, s + NS, slot);
                 }
             }
+            if (SHIFT)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) by[0][j] = by[1][j];
             slot = next;
         }
         wait_vmcnt<0>();                                   // no copy is under way when the workgroup gives its LDS back
@@ -257,13 +289,15 @@ product_kernel(ProductArgs p, typename Epilogue::Args e) {
     Epilogue::template run<FM, FN>(e, smem, acc, m0 + ma, n0 + nb, split, n);
 }
 
-template <class Sh, int AK, int BK, class Epilogue, int CUTS = 0>
+template <class Sh, int AK, int BK, class Epilogue, int CUTS = 0, bool SHIFT = false>
 static qless_status launch_product(const ProductArgs &p, const typename Epilogue::Args &e, hipStream_t st) {
-    QLESS_LDS_KERNEL((product_kernel<Sh, AK, BK, Epilogue, CUTS>), Sh::LDS);
+    constexpr int LDS = Sh::LDS + (SHIFT ? Sh::NS * Sh::NW * 256 : 0);
+    static_assert(LDS <= 160 * 1024, "the stages fit");
+    QLESS_LDS_KERNEL((product_kernel<Sh, AK, BK, Epilogue, CUTS, SHIFT>), LDS);
     const int64_t total = p.mtiles * ((p.n + Sh::NT - 1) / Sh::NT) * p.splits, grid = (total + 7) / 8 * 8;
     if (grid > 0x7FFFFFFF) return QLESS_ERR_UNSUPPORTED;
     if (grid > 0)
-        hipLaunchKernelGGL((product_kernel<Sh, AK, BK, Epilogue, CUTS>), dim3((unsigned)grid), dim3(64 * Sh::NW), Sh::LDS, st, p, e);
+        hipLaunchKernelGGL((product_kernel<Sh, AK, BK, Epilogue, CUTS, SHIFT>), dim3((unsigned)grid), dim3(64 * Sh::NW), LDS, st, p, e);
     return QLESS_OK;
 }
 

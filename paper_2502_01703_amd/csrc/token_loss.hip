@@ -6,10 +6,13 @@
 // on the device), so that a prompt costs no products.
 //
 // Loss alone: the tiles of logits end with the maximum and the sum of their exponentials, which are joined.
-// dH: a piece of the vocabulary at a time, the logits of the piece (fp32, in the workspace, small enough to stay in the last-level cache)
-// become p = exp(z - m) with the running maximum m, and planes = planes exp(m_before - m) + p W: one pass over the vocabulary, as with
-// the running softmax of an attention.  dH = w / s planes + w (p_target - 1) W_target at the end.
-// dW needs lse first.  Where the whole vocabulary is one piece, delta is final at once; else a second pass forms the logits again.
+// dH: a piece of the vocabulary at a time, one pass over it, as with the running softmax of an attention: planes = planes 2^(R_before - R) +
+// p W, dH = w / s planes + w (p_target - 1) W_target at the end.  The tiles end with p = 2^(z log2 e - r), r the whole number above their
+// own maximum, as bfloat16, with the sum of the others' p in fp32; a small kernel finds R, the greatest r of a token so far; and
+// the product with W takes 2^(r - R) off the exponents of its operand, exactly.  So the logits are never in memory, and p is
+// rounded once.  (With fp32 logits in memory and a kernel that turned them into p, 4096 x 4096 x 131072 took 7.9 ms.)
+// dW needs the sums first, and its operand's factors are not of its entries but of its tokens.  Where the whole vocabulary is one piece,
+// its logits are kept until delta is formed from them; else a second pass forms them again.
 //
 // The target's entry, the largest of a row, never passes through the bfloat16 operand: it is added in fp32, to dH in the last kernel,
 // to dW behind the product, from the tokens ordered by target.  (Rounded with the rest it made gradients of few tokens up to 0.4 %
@@ -17,6 +20,7 @@
 #include "product.h"
 #include "score.h"
 #include "token_loss.h"
+#include <type_traits>
 
 namespace qless {
 
@@ -26,9 +30,10 @@ struct LossTokens {                        // workspace views, by live token (pa
     int32_t *token, *target;               // [Tp]
     int32_t *place;                        // [T]: live index of a token, or -1
     float *weight, *lse, *hit;             // [Tp]; hit: the target's logit
-    float *top, *sum, *shrink;             // [Tp] running maximum and sum; exp of the last change of the maximum
+    float *top, *sum, *shrink;             // [Tp] R, sum of the others' 2^(z log2 e - R), 2^ the last change of R (few tokens: of exp and m)
     float *pull;                           // [Tp] w (p_target - 1)
-    float2 *part;                          // [parts][Tp] maximum, sum of exp(z - maximum)
+    float2 *part;                          // [parts][Tp] maximum, sum of exp(z - maximum); or r, sum of the others' p
+    uint32_t *shift;                       // [parts][Tp] R - r, for two exponents
     int32_t *order, *order_target, *start; // [Tp] live tokens by target, and their targets; [Vp / 64 + 1]: where each 64 entries begin there
     float *logits;                         // [Tp][piece]
     uint16_t *delta;                       // [Tp][piece]
@@ -40,7 +45,7 @@ struct LossPlan {
     int64_t T, Tp, Dp, Vp, piece, parts;
     int32_t D, V, tile_n, tile_m, splits, raw;
     bool one_pass;                         // dW without a second pass
-    size_t off[19], total;
+    size_t off[20], total;
 };
 
 constexpr int kGather = 1024;              // entries of a part where partial logits are added
@@ -143,12 +148,12 @@ loss_rows_kernel(const uint16_t *X, int64_t ldX, int32_t D, const int32_t *from,
     }
 }
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 __device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // ---- what the tiles of logits end with: rows m are vocabulary entries, columns n tokens
-// STORE: the logits too, for a delta kernel; SUM: the exponentials (else that kernel forms them)
-template <bool STORE, bool SUM> struct LossStats {
+// STORE: the logits too, for a delta kernel
+template <bool STORE> struct LossStats {
     struct Args { const int32_t *target; float *hit; float2 *part; int64_t Tp, first; int32_t V; float *logits; int64_t ld; };
     template <int FM, int FN>
     static __device__ inline void run(const Args &a, unsigned char *lds, f32x16 (&acc)[FM][FN], int64_t m, int64_t n, int, int64_t live) {
@@ -180,21 +185,76 @@ template <bool STORE, bool SUM> struct LossStats {
 #pragma unroll
                 for (int v = 0; v < 16; ++v) top = fmaxf(top, acc[i][j][v]);
             top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float ref = (top == -INFINITY ? 0.0f : top) * kLog2e;
             float sum = 0.0f;
-            if (SUM) {
-                const float ref = (top == -INFINITY ? 0.0f : top) * kLog2e;
 #pragma unroll
-                for (int i = 0; i < FM; ++i)
+            for (int i = 0; i < FM; ++i)
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) sum += exp2_of(__builtin_fmaf(acc[i][j][v], kLog2e, -ref));
-                sum += __shfl_xor(sum, 32, 64);
-            }
+                for (int v = 0; v < 16; ++v) sum += exp2_of(__builtin_fmaf(acc[i][j][v], kLog2e, -ref));
+            sum += __shfl_xor(sum, 32, 64);
             if (half == 0 && t < live) a.part[part * a.Tp + t] = make_float2(top, sum);
         }
         if (STORE)
             by_rows<FM, FN>(lds, acc, [&](int r, int c, f32x4 x) {
                 if (n + r < live) *(f32x4 *)(a.logits + (n + r) * a.ld + m + c) = x;
             });
+    }
+};
+
+// p = 2^(z log2 e - r) of a piece, without the targets' entries, as bfloat16, r and the sums
+struct LossPower {
+    struct Args { const int32_t *target; float *hit; float2 *part; int64_t Tp, first; int32_t V; uint16_t *out; int64_t ld; };
+    template <int FM, int FN>
+    static __device__ inline void run(const Args &a, unsigned char *lds, f32x16 (&acc)[FM][FN], int64_t m, int64_t n, int, int64_t live) {
+        const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
+        const int v0 = (int)(a.first + m) + 4 * half, over = a.V - v0;         // entries from here on
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const int64_t t = n + 32 * j + l32;
+            const int y = t < live ? a.target[t] - v0 : -1;
+            const bool here = y >= 0 && y < 32 * FM && (y & 4) == 0;
+            if (over < 32 * FM) {                           // the end of the vocabulary
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) acc[i][j][v] = 32 * i + 8 * (v >> 2) + (v & 3) < over ? acc[i][j][v] : -INFINITY;
+            }
+            float top = acc[0][j][0];
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) top = fmaxf(top, acc[i][j][v]);
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float r = top == -INFINITY ? 0.0f : ceilf(top * kLog2e);
+            if (__any(here)) {
+                float hit = 0.0f;
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const bool it = y == 32 * i + 8 * (v >> 2) + (v & 3);
+                        hit = it ? acc[i][j][v] : hit;
+                        acc[i][j][v] = it ? -INFINITY : acc[i][j][v];
+                    }
+                if (here) a.hit[t] = hit;
+            }
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    acc[i][j][v] = exp2_of(__builtin_fmaf(acc[i][j][v], kLog2e, -r));
+                    sum += acc[i][j][v];
+                }
+            sum += __shfl_xor(sum, 32, 64);
+            if (half == 0 && t < live) a.part[m / (32 * FM) * a.Tp + t] = make_float2(top == -INFINITY ? -INFINITY : r, sum);
+        }
+        by_rows<FM, FN>(lds, acc, [&](int row, int c, f32x4 x) {
+            uint16_t d[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) d[u] = __builtin_bit_cast(uint16_t, (__bf16)x[u]);
+            if (n + row < live) __builtin_memcpy(__builtin_assume_aligned(a.out + (n + row) * a.ld + m + c, 8), d, 8);
+        });
     }
 };
 
@@ -430,7 +490,8 @@ loss_delta_kernel(LossTokens w, int64_t Tp, int64_t parts, int64_t first, int64_
 }
 
 // Partial logits added, with what the tiles' epilogue leaves of whole ones: a workgroup kGather entries of a token.
-template <bool STORE>
+enum { SUMS = 0, LOGITS = 1, POWERS = 2 };
+template <int WHAT>
 __global__ void __launch_bounds__(256)
 loss_gather_kernel(LossTokens w, int64_t Tp, int64_t Vp, int raw, int32_t V) {
     __shared__ float s_top[4], s_sum[4];
@@ -448,7 +509,7 @@ loss_gather_kernel(LossTokens w, int64_t Tp, int64_t Vp, int raw, int32_t V) {
             if (u == y) w.hit[t] = z[u];
             if (c + u >= V) z[u] = -INFINITY;
         }
-        if (STORE) *(f32x4 *)(w.logits + t * Vp + c) = z;
+        if (WHAT == LOGITS) *(f32x4 *)(w.logits + t * Vp + c) = z;
     }
     float top = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]));
 #pragma unroll
@@ -456,13 +517,66 @@ loss_gather_kernel(LossTokens w, int64_t Tp, int64_t Vp, int raw, int32_t V) {
     if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = top;
     __syncthreads();
     top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
-    const float ref = top == -INFINITY ? 0.0f : top;
-    float sum = (__expf(z[0] - ref) + __expf(z[1] - ref)) + (__expf(z[2] - ref) + __expf(z[3] - ref));
+    float ref = top == -INFINITY ? 0.0f : top, p[4];
+    if (WHAT == POWERS) ref = ceilf(ref * kLog2e);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        if (WHAT == POWERS) p[u] = w.target[t] == c + u ? 0.0f : exp2_of(__builtin_fmaf(z[u], kLog2e, -ref));
+        else p[u] = __expf(z[u] - ref);
+    }
+    if (WHAT == POWERS && c < Vp) {
+        uint16_t d[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) d[u] = __builtin_bit_cast(uint16_t, (__bf16)p[u]);
+        __builtin_memcpy(__builtin_assume_aligned(w.delta + t * Vp + c, 8), d, 8);
+    }
+    float sum = (p[0] + p[1]) + (p[2] + p[3]);
 #pragma unroll
     for (int d = 32; d > 0; d /= 2) sum += __shfl_xor(sum, d, 64);
     if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) w.part[(int64_t)blockIdx.y * Tp + t] = make_float2(top, (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]));
+    if (threadIdx.x == 0) w.part[(int64_t)blockIdx.y * Tp + t] = make_float2(WHAT == POWERS && top != -INFINITY ? ref : top, (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]));
+}
+
+// R of a piece: TOK tokens a workgroup.  Where the maximum is not a number's, the sum is not one either.
+template <int TOK>
+__global__ void __launch_bounds__(1024)
+loss_shift_kernel(LossTokens w, int64_t Tp, int64_t parts, int first) {
+    constexpr int LANES = 1024 / TOK, WAVES = 16;           // a wavefront's 64 / TOK threads of a token are joined in registers
+    __shared__ float s_top[WAVES][TOK], s_sum[WAVES][TOK];
+    const int64_t live = *w.count, t = (int64_t)blockIdx.x * TOK + threadIdx.x % TOK;
+    if ((int64_t)blockIdx.x * TOK >= live) return;          // the whole workgroup
+    const int lane = threadIdx.x / TOK, tok = threadIdx.x % TOK, wave = threadIdx.x >> 6;
+    const int64_t mine = t < live ? parts : 0;
+    const float before = t < live && !first ? w.top[t] : -INFINITY;
+    float top = before;
+#pragma unroll 4
+    for (int64_t p = lane; p < mine; p += LANES) top = fmaxf(top, w.part[p * Tp + t].x);
+#pragma unroll
+    for (int d = TOK; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
+    if ((threadIdx.x & 63) < TOK) s_top[wave][tok] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) top = fmaxf(top, s_top[i][tok]);
+    float sum = 0.0f;
+#pragma unroll 4
+    for (int64_t p = lane; p < mine; p += LANES) {
+        const float2 x = w.part[p * Tp + t];
+        const float by = fminf(top - x.x, 255.0f);          // of a part without entries, or numbers: 255
+        sum += x.y * exp2_of(x.x - top);
+        w.shift[p * Tp + t] = (uint32_t)(int)by * 0x00800080u;
+    }
+#pragma unroll
+    for (int d = TOK; d < 64; d *= 2) sum += __shfl_xor(sum, d, 64);
+    if ((threadIdx.x & 63) < TOK) s_sum[wave][tok] = sum;
+    __syncthreads();
+    if (lane == 0 && t < live) {
+        for (int i = 1; i < WAVES; ++i) sum += s_sum[i][tok];
+        const float shrink = before == -INFINITY ? 0.0f : exp2_of(before - top);
+        w.top[t] = top;
+        w.sum[t] = (first ? 0.0f : w.sum[t] * shrink) + sum;
+        w.shrink[t] = shrink;
+    }
 }
 
 // The live tokens in the order of target and token, and where each 64 vocabulary entries begin there: 16 threads count what comes before
@@ -503,11 +617,21 @@ loss_hidden_kernel(LossTokens w, int64_t Tp, int64_t Dp, int32_t D, int splits, 
     if (r >= 0) {
         row += w.target[r] * ldW;
         if (run) {
-            const float top = w.top[r], sum = w.sum[r], one = loss_of(top, sum, w.hit[r]);
-            scale = w.weight[r] / sum;
-            pull = w.weight[r] * expm1f(-one);
+            float one, all;
+            if (run == 2) {                                 // powers of two, the target apart: small losses and 1 - p_target keep their digits
+                const float top = w.top[r], others = w.sum[r], at = __builtin_fmaf(w.hit[r], kLog2e, -top), mine = exp2_of(at), total = others + mine;
+                one = others < mine ? log1pf(others / mine) : kLn2 * (log2f(total) - at);
+                all = one + w.hit[r];
+                scale = w.weight[r] / total;
+                pull = -scale * others;
+            } else {
+                const float top = w.top[r], sum = w.sum[r];
+                one = loss_of(top, sum, w.hit[r]);
+                all = top + logf(sum);
+                scale = w.weight[r] / sum;
+                pull = w.weight[r] * expm1f(-one);
+            }
             if (threadIdx.x == 0 && blockIdx.y == 0) {
-                const float all = top + logf(sum);
                 nll[t] = one;
                 if (lse) lse[t] = all;
                 w.lse[r] = all;
@@ -561,7 +685,9 @@ loss_hidden_kernel(LossTokens w, int64_t Tp, int64_t Dp, int32_t D, int splits, 
 typedef ProductShape<256, 256, 2, 4, 2> Loss256;
 typedef ProductShape<128, 256, 2, 4, 3> LossHalf;
 typedef ProductShape<256, 128, 4, 2, 3> Loss128;
-typedef ProductShape<256, 64, 8, 1, 4> Loss64;
+typedef ProductShape<256, 64, 4, 2, 4> Loss64;
+typedef ProductShape<256, 64, 4, 2, 3> LossShift;          // with room for shifts
+typedef ProductShape<256, 64, 8, 1, 4> LossTerms;          // both terms of few tokens in a wavefront
 typedef ProductShape<256, 32, 8, 1, 4> Loss32;
 typedef ProductShape<128, 128, 2, 2, 2> LossSmall;         // dW where larger tiles do not fill the chip
 
@@ -576,8 +702,8 @@ static LossPlan loss_plan(int64_t T, int32_t D, int32_t V, bool want_dH, bool wa
     p.Dp = up_to(D, 64);
     p.Vp = up_to(V, 256);
     const bool gradient = want_dH || want_dW;
-    // A piece: logits and delta of up to 1.5 GB.  (Their 10 bytes a logit come from memory at any size that is worth its additions to
-    // the planes, and more tiles fill their last round better.)  With dW one piece saves the second pass.  Few tokens: one piece.
+    // A piece: p, or logits and delta, of up to 1.5 GB (they come from memory at any size that is worth its additions to the planes, and more
+    // tiles fill their last round better).  With dW one piece saves the second pass.  Few tokens: one piece.
     const int64_t budget = (int64_t)1536 << 20, cus = compute_units();
     const int64_t ntiles = (T + p.tile_n - 1) / p.tile_n;
     // The tiles of logits where few fill the chip: rounds of tiles of 128 entries, at 0.64 of the larger ones' time each (256 x 4096 x 32000,
@@ -597,11 +723,12 @@ static LossPlan loss_plan(int64_t T, int32_t D, int32_t V, bool want_dH, bool wa
         p.tile_m = 256;
     }
     p.parts = p.Vp / 32;                                    // at most (32 entries a part)
-    p.one_pass = T <= kFew || p.Tp * p.Vp * 6 <= budget;
+    p.one_pass = T <= kFew || (want_dW && p.Tp * p.Vp * 6 <= budget);
+    const int64_t bytes = p.one_pass ? 6 : 2;               // of an entry of a piece
     int64_t piece = p.Vp;
-    if (!p.one_pass) {
+    if (!p.one_pass && p.Tp * p.Vp * bytes > budget) {
         // whole rounds of tiles of the chip, if all tokens are live
-        int64_t m = budget / (6 * p.Tp) / 256;
+        int64_t m = budget / (bytes * p.Tp) / 256;
         if (m < 8) m = 8;
         const int64_t rounds = m * ntiles / cus;
         if (rounds > 0) m = rounds * cus / ntiles > 0 ? rounds * cus / ntiles : 1;
@@ -623,33 +750,37 @@ static LossPlan loss_plan(int64_t T, int32_t D, int32_t V, bool want_dH, bool wa
     take((size_t)p.parts * p.Tp * 8);                       // 12 part
     take(want_dW ? (size_t)p.Tp * 8 : 0);                   // 13 order, order_target
     take(want_dW ? (size_t)(p.Vp / 64 + 1) * 4 : 0);        // 14 start
-    // 15: a piece's logits and delta; where W has to be packed, shorter pieces with the packed rows behind them: room for 64 MB of all three
-    const size_t each = (size_t)p.Tp * (gradient ? 6 : 0) + (size_t)p.Dp * 2;
-    size_t whole = gradient ? (size_t)p.Tp * piece * 6 : 0, packed = each * p.Vp;
+    // 15: a piece's logits and delta, or p; where W has to be packed, shorter pieces with the packed rows behind them: room for 64 MB of them all
+    const size_t each = (size_t)p.Tp * (gradient ? bytes : 0) + (size_t)p.Dp * 2;
+    size_t whole = gradient ? (size_t)p.Tp * piece * bytes : 0, packed = each * p.Vp;
     if (packed > ((size_t)64 << 20)) packed = (size_t)64 << 20;
     if (packed < each * 256) packed = each * 256;
     take(whole > packed ? whole : packed);
     take(want_dH ? (size_t)p.splits * p.Tp * p.Dp * 4 : 0); // 16 planes
     take(p.raw > 1 ? (size_t)p.raw * p.Tp * p.Vp * 4 : 0);  // 17 raw
+    take(want_dH && T > kFew ? (size_t)(piece / 64) * p.Tp * 4 : 0);      // 18 shift
     p.total = at;
     return p;
 }
 
-template <class Epilogue, int AK, int BK>
+// FROM: the smallest tile that a call takes
+template <class Epilogue, int AK, int BK, int FROM, bool SHIFT = false>
 static qless_status loss_product(int tile_n, const ProductArgs &a, const typename Epilogue::Args &e, hipStream_t st) {
     switch (tile_n) {
-        case 32: return launch_product<Loss32, AK, BK, Epilogue>(a, e, st);
-        case 64: return launch_product<Loss64, AK, BK, Epilogue>(a, e, st);
-        case 128: return launch_product<Loss128, AK, BK, Epilogue>(a, e, st);
-        default: return launch_product<Loss256, AK, BK, Epilogue>(a, e, st);
+        case 32:
+            if constexpr (FROM == 32) return launch_product<Loss32, AK, BK, Epilogue>(a, e, st);
+            return QLESS_ERR_UNSUPPORTED;
+        case 64: return launch_product<std::conditional_t<SHIFT, LossShift, Loss64>, AK, BK, Epilogue, 0, SHIFT>(a, e, st);
+        case 128: return launch_product<Loss128, AK, BK, Epilogue, 0, SHIFT>(a, e, st);
+        default: return launch_product<Loss256, AK, BK, Epilogue, 0, SHIFT>(a, e, st);
     }
 }
 // the tiles of logits of `entries` from the vocabulary
-template <class Epilogue>
+template <class Epilogue, int FROM>
 static qless_status logits_product(const LossPlan &p, ProductArgs a, int64_t entries, const typename Epilogue::Args &e, hipStream_t st) {
     a.mtiles = (int32_t)((entries + p.tile_m - 1) / p.tile_m);
     if (p.tile_m == 128) return launch_product<LossHalf, ALONG, ALONG, Epilogue>(a, e, st);
-    return loss_product<Epilogue, ALONG, ALONG>(p.tile_n, a, e, st);
+    return loss_product<Epilogue, ALONG, ALONG, FROM>(p.tile_n, a, e, st);
 }
 
 }  // namespace qless
@@ -686,17 +817,19 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
     w.token = ints(2); w.target = ints(3); w.place = ints(4);
     w.weight = floats(5); w.lse = floats(6); w.hit = floats(7); w.top = floats(8); w.sum = floats(9); w.shrink = floats(10); w.pull = floats(11);
     w.part = (float2 *)(base + p.off[12]); w.order = ints(13); w.order_target = w.order + p.Tp; w.start = ints(14);
-    w.logits = floats(15); w.planes = floats(16); w.raw = floats(17);
+    w.logits = floats(15); w.planes = floats(16); w.raw = floats(17); w.shift = (uint32_t *)ints(18);
 
     const bool gradient = dH || dW, few = T <= kFew;
+    const int64_t bytes = p.one_pass ? 6 : 2;
     int64_t piece = gradient ? p.piece : p.Vp;
     if (packs) {
-        const int64_t room = (int64_t)((p.off[16] - p.off[15]) / ((size_t)p.Tp * (gradient ? 6 : 0) + (size_t)p.Dp * 2)) / 256 * 256;
+        const int64_t room = (int64_t)((p.off[16] - p.off[15]) / ((size_t)p.Tp * (gradient ? bytes : 0) + (size_t)p.Dp * 2)) / 256 * 256;
         if (piece > room) piece = room;
     }
-    const bool one_pass = gradient && piece == p.Vp;
-    w.delta = (uint16_t *)(w.logits + p.Tp * piece);
-    w.pack = gradient ? w.delta + p.Tp * piece : (uint16_t *)w.logits;
+    // Where dW was to need no second pass but W is packed, its pieces are the plan's pieces' part: dH runs along powers of two then too.
+    const bool one_pass = gradient && p.one_pass && piece == p.Vp, power = dH && !few && !one_pass;
+    w.delta = few || one_pass ? (uint16_t *)(w.logits + p.Tp * piece) : (uint16_t *)w.logits;
+    w.pack = gradient ? (uint16_t *)((unsigned char *)w.logits + p.Tp * piece * bytes) : (uint16_t *)w.logits;
     auto rows_of = [&](int64_t v0) { return V - v0 < piece ? V - v0 : piece; };
     auto head = [&](int64_t v0) {                           // a piece of W by rows of D
         if (!packs) return ProductOperand{(const uint16_t *)W + v0 * ldW, V > 1 ? ldW * 2 : p.Dp * 2, rows_of(v0), (int64_t)D * 2};
@@ -705,15 +838,21 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
         return ProductOperand{w.pack, p.Dp * 2, n, p.Dp * 2};
     };
     const ProductOperand tokens{w.H, p.Dp * 2, p.Tp, p.Dp * 2};
+    const bool raw = p.raw > 1 && piece == p.Vp;
+    const int per_part = raw ? kGather : p.tile_m == 128 ? 64 : p.tile_n == 256 ? 128 : p.tile_n == 32 ? 32 : 64;
+    auto parts_of = [&](int64_t entries) { return (entries + per_part - 1) / per_part; };
     auto hidden_product = [&](const ProductOperand &rows, int64_t n, int64_t v0) {        // dH's planes: rows m columns of W, columns n tokens
-        ProductArgs a{ProductOperand{rows.base, rows.ld, rows.depth, n}, ProductOperand{w.delta, piece * 2, few ? 2 * kFew : p.Tp, up_to(n, 64) * 2},
-                      few ? 2 * kFew : T, n, few ? nullptr : w.count, nullptr, (D + 255) / 256, p.splits};
-        if (few) return launch_product<Loss64, ACROSS, ALONG, LossPlane<true>>(a, LossPlane<true>::Args{w.planes, p.Tp, p.Dp, v0 > 0 ? w.shrink : nullptr}, st);
-        return loss_product<LossPlane<false>, ACROSS, ALONG>(p.tile_n, a, LossPlane<false>::Args{w.planes, p.Tp, p.Dp, v0 > 0 ? w.shrink : nullptr}, st);
+        const ProductArgs a{ProductOperand{rows.base, rows.ld, rows.depth, n}, ProductOperand{w.delta, piece * 2, few ? 2 * kFew : p.Tp, up_to(n, 64) * 2},
+                            few ? 2 * kFew : T, n, few ? nullptr : w.count, nullptr, (D + 255) / 256, p.splits, nullptr,
+                            w.shift, p.Tp, raw ? 4 : per_part == 128 ? 1 : 0};
+        const float *shrink = v0 > 0 ? w.shrink : nullptr;
+        if (few) return launch_product<LossTerms, ACROSS, ALONG, LossPlane<true>>(a, LossPlane<true>::Args{w.planes, p.Tp, p.Dp, shrink}, st);
+        const LossPlane<false>::Args e{w.planes, p.Tp, p.Dp, shrink};
+        return power ? loss_product<LossPlane<false>, ACROSS, ALONG, 64, true>(p.tile_n, a, e, st) : loss_product<LossPlane<false>, ACROSS, ALONG, 64>(p.tile_n, a, e, st);
     };
     auto head_product = [&](int64_t n, int64_t v0) {        // dW: rows m columns of H, columns n entries
         ProductArgs a{ProductOperand{w.H, p.Dp * 2, p.Dp * 2, p.Tp}, ProductOperand{w.delta, piece * 2, up_to(n, 64) * 2, few ? 2 * kFew : p.Tp},
-                      n, T == 0 ? 0 : few ? 2 * kFew : p.Tp, nullptr, few ? nullptr : w.count, (D + 255) / 256, 1};
+                      n, T == 0 ? 0 : few ? 2 * kFew : p.Tp, nullptr, few ? nullptr : w.count, (D + 255) / 256, 1, nullptr, nullptr, 0, 0};
         const LossHead::Args e{(uint16_t *)dW, ldDW, v0, V, D, w.order, w.order_target, w.start, w.pull, w.H, p.Dp};
         if (a.mtiles * ((n + 255) / 256) < compute_units()) {            // 512 x 512 x 2000: 104 -> 86 us; a chip full of the larger ones is 5 % faster
             a.mtiles = (D + 127) / 128;
@@ -731,43 +870,40 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
     if (dW)
         hipLaunchKernelGGL(loss_order_kernel, dim3((unsigned)((T + 15) / 16 + (p.Vp / 64 + 1 + 15) / 16)), dim3(256), 0, st, w, T, p.Vp / 64 + 1);
     qless_status rc = QLESS_OK;
-    const bool raw = p.raw > 1 && piece == p.Vp;
-    const int per_part = raw ? kGather : p.tile_m == 128 ? 64 : p.tile_n == 256 ? 128 : p.tile_n == 128 ? 64 : 32;
-    auto parts_of = [&](int64_t entries) { return (entries + per_part - 1) / per_part; };
-
     // first pass: the losses, and dH unless delta comes with dW
-    const bool run = dH && (!one_pass || (!dW && T >= 256));    // (fewer tokens: their rows are shared out, which takes lse first)
-    const bool store = dH || one_pass;
+    const bool run = few && dH && !one_pass, store = one_pass || run;
     for (int64_t v0 = 0; T > 0 && v0 < V && rc == QLESS_OK; v0 += piece) {
-        const int64_t n = rows_of(v0), np = up_to(n, 256);
+        const int64_t n = rows_of(v0), np = up_to(n, 256), parts = parts_of(np);
         const ProductOperand rows = head(v0);
-        const ProductArgs a{rows, tokens, T, p.Dp, w.count, nullptr, 0, raw ? p.raw : 1, nullptr};
+        const ProductArgs a{rows, tokens, T, p.Dp, w.count, nullptr, 0, raw ? p.raw : 1, nullptr, nullptr, 0, 0};
         if (raw) {
-            rc = logits_product<LossPlane<false>>(p, a, np, LossPlane<false>::Args{w.raw, p.Tp, p.Vp, nullptr}, st);
-            const dim3 grid((unsigned)T, (unsigned)parts_of(p.Vp));
-            if (store) hipLaunchKernelGGL(loss_gather_kernel<true>, grid, dim3(256), 0, st, w, p.Tp, p.Vp, p.raw, V);
-            else hipLaunchKernelGGL(loss_gather_kernel<false>, grid, dim3(256), 0, st, w, p.Tp, p.Vp, p.raw, V);
-        } else if (!store) {
-            rc = logits_product<LossStats<false, true>>(p, a, np, LossStats<false, true>::Args{w.target, w.hit, w.part, p.Tp, v0, V, nullptr, 0}, st);
-        } else if (run) {
-            rc = logits_product<LossStats<true, false>>(p, a, np, LossStats<true, false>::Args{w.target, w.hit, w.part, p.Tp, v0, V, w.logits, piece}, st);
+            rc = logits_product<LossPlane<false>, 32>(p, a, np, LossPlane<false>::Args{w.raw, p.Tp, p.Vp, nullptr}, st);
+            auto gather = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)T, (unsigned)parts), dim3(256), 0, st, w, p.Tp, p.Vp, p.raw, V); };
+            power ? gather(loss_gather_kernel<POWERS>) : store ? gather(loss_gather_kernel<LOGITS>) : gather(loss_gather_kernel<SUMS>);
+        } else if (power) {
+            rc = logits_product<LossPower, 64>(p, a, np, LossPower::Args{w.target, w.hit, w.part, p.Tp, v0, V, w.delta, piece}, st);
+        } else if (store) {
+            rc = logits_product<LossStats<true>, 32>(p, a, np, LossStats<true>::Args{w.target, w.hit, w.part, p.Tp, v0, V, w.logits, piece}, st);
         } else {
-            rc = logits_product<LossStats<true, true>>(p, a, np, LossStats<true, true>::Args{w.target, w.hit, w.part, p.Tp, v0, V, w.logits, piece}, st);
+            rc = logits_product<LossStats<false>, 32>(p, a, np, LossStats<false>::Args{w.target, w.hit, w.part, p.Tp, v0, V, nullptr, 0}, st);
         }
-        if (!store) continue;
         if (rc != QLESS_OK) break;
-        int64_t shares = run || T >= 1024 ? 1 : 1024 / T + 1;                  // of a row
-        if (shares > np / 1024) shares = np / 1024 > 0 ? np / 1024 : 1;
-        const dim3 grid((unsigned)up_to(T, few ? kFew : 64), (unsigned)shares);
-        const int64_t parts = parts_of(np);
-        auto delta = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, w, p.Tp, parts, v0, np, piece, nll, lse); };
-        if (run) few ? delta(loss_delta_kernel<true, true>) : delta(loss_delta_kernel<true, false>);
-        else few ? delta(loss_delta_kernel<false, true>) : delta(loss_delta_kernel<false, false>);
+        if (power) {
+            if (T <= 1024) hipLaunchKernelGGL(loss_shift_kernel<4>, dim3((unsigned)((T + 3) / 4)), dim3(1024), 0, st, w, p.Tp, parts, v0 == 0 ? 1 : 0);
+            else hipLaunchKernelGGL(loss_shift_kernel<16>, dim3((unsigned)((T + 15) / 16)), dim3(1024), 0, st, w, p.Tp, parts, v0 == 0 ? 1 : 0);
+        } else if (store) {
+            int64_t shares = run || T >= 1024 ? 1 : 1024 / T + 1;              // of a row
+            if (shares > np / 1024) shares = np / 1024 > 0 ? np / 1024 : 1;
+            auto delta = [&](auto kernel) {
+                hipLaunchKernelGGL(kernel, dim3((unsigned)up_to(T, few ? kFew : 64), (unsigned)shares), dim3(256), 0, st, w, p.Tp, parts, v0, np, piece, nll, lse);
+            };
+            run ? delta(loss_delta_kernel<true, true>) : few ? delta(loss_delta_kernel<false, true>) : delta(loss_delta_kernel<false, false>);
+        }
         if (dH) rc = hidden_product(rows, n, v0);
         if (rc == QLESS_OK && dW && one_pass) rc = head_product(n, v0);
     }
     if (rc != QLESS_OK) return rc;
-    if (T > 0 && !store) {
+    if (T > 0 && !store && !power) {
         const int64_t parts = parts_of(p.Vp);
         if (T <= 64) hipLaunchKernelGGL(loss_join_kernel<1>, dim3((unsigned)T), dim3(256), 0, st, w, p.Tp, parts, nll, lse);
         else hipLaunchKernelGGL(loss_join_kernel<4>, dim3((unsigned)((T + 3) / 4)), dim3(256), 0, st, w, p.Tp, parts, nll, lse);
@@ -776,7 +912,7 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
         auto hidden = [&](auto kernel, int cols) {
             int64_t shares = 2048 / T + 1;
             if (shares > (D + cols - 1) / cols) shares = (D + cols - 1) / cols;
-            hipLaunchKernelGGL(kernel, dim3((unsigned)T, (unsigned)shares), dim3(256), 0, st, w, p.Tp, p.Dp, D, p.splits, run ? 1 : 0, (const uint16_t *)W, ldW, (uint16_t *)dH, ldDH, nll, lse);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)T, (unsigned)shares), dim3(256), 0, st, w, p.Tp, p.Dp, D, p.splits, power ? 2 : run ? 1 : 0, (const uint16_t *)W, ldW, (uint16_t *)dH, ldDH, nll, lse);
         };
         if (p.splits >= 16) hidden(loss_hidden_kernel<16>, 64);
         else if (p.splits >= 4) hidden(loss_hidden_kernel<4>, 256);
@@ -786,9 +922,9 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
     // second pass: delta from the known losses, a piece at a time, and dW
     for (int64_t v0 = 0; dW && (!one_pass || T == 0) && v0 < V && rc == QLESS_OK; v0 += piece) {
         const int64_t n = rows_of(v0);
-        const ProductArgs a{head(v0), tokens, T, p.Dp, w.count, nullptr, (int32_t)(up_to(n, 256) / 256), 1, nullptr};
+        const ProductArgs a{head(v0), tokens, T, p.Dp, w.count, nullptr, (int32_t)(up_to(n, 256) / 256), 1, nullptr, nullptr, 0, 0};
         if (few) rc = launch_product<Loss32, ALONG, ALONG, LossDelta<true>>(a, LossDelta<true>::Args{w.target, w.lse, w.weight, w.delta, piece, v0, V}, st);
-        else rc = loss_product<LossDelta<false>, ALONG, ALONG>(p.tile_n, a, LossDelta<false>::Args{w.target, w.lse, w.weight, w.delta, piece, v0, V}, st);
+        else rc = loss_product<LossDelta<false>, ALONG, ALONG, 64>(p.tile_n, a, LossDelta<false>::Args{w.target, w.lse, w.weight, w.delta, piece, v0, V}, st);
         if (rc == QLESS_OK) rc = head_product(n, v0);
     }
     return rc == QLESS_OK ? launch_status() : rc;

@@ -140,6 +140,36 @@ def test_pieces_of_the_vocabulary(T, D, V):
     _check(H, W, y, w, Q.token_loss(H, W, y, w, want_dW=True))
 
 
+@pytest.mark.parametrize("want_dW", [False, True])
+def test_pieces_read_in_place(want_dW):
+    """Several pieces of a vocabulary that needs no packing, for dH alone and with dW."""
+    _say("loss pieces read in place dW=%s" % want_dW)
+    H, W, y, w = _inputs(9000, 40, 100000, 11, masked=0.2)
+    _check(H, W, y, w, Q.token_loss(H, W, y, w, want_dW=want_dW))
+
+
+@pytest.mark.parametrize("T,D,V", [(130, 256, 1000), (700, 128, 9000), (9000, 40, 100000)])
+@pytest.mark.parametrize("rise", [-1.0, 1.0])
+def test_logits_that_rise_over_the_vocabulary(T, D, V, rise):
+    """The greatest logit so far changes from part to part, by more than the range of an exponent over the whole."""
+    _say("loss with rising logits T=%d rise=%g" % (T, rise))
+    H, W, y, w = _inputs(T, D, V, 12, masked=0.2)
+    H[:, 0] = torch.linspace(0, 8, T, device=DEV).bfloat16()
+    W[:, 0] = (rise * torch.linspace(-40, 40, V, device=DEV)).bfloat16()
+    _check(H, W, y, w, Q.token_loss(H, W, y, w))
+
+
+@pytest.mark.parametrize("scale", [0.0, 60.0, 3000.0])
+@pytest.mark.parametrize("T", [50, 400])
+def test_certain_and_hopeless_tokens_for_dH(T, scale):
+    _say("loss scale %g T=%d, dH alone" % (scale, T))
+    H, W, y, w = _inputs(T, 256, 1000, 6, masked=0.1, scale=scale)
+    H[::3] = -H[::3]
+    _check(H, W, y, w, Q.token_loss(H, W, y, w))
+    y[:] = 999
+    _check(H, W, y, w, Q.token_loss(H, W, y, w))
+
+
 @pytest.mark.parametrize("T", [3, 100])
 def test_no_target_at_all(T):
     _say("loss without targets T=%d" % T)
