@@ -170,9 +170,9 @@ checkpoint_read_kernel(const int8_t *codes, int64_t ldC, const float *step, int6
 // An example longer than `chunk` tokens is cut into segments of that many.  With phi(e) = e + floor(offset[e] / chunk), the numbers
 // phi(e) .. phi(e + 1) - 1 suffice for those of example e (one may be left over), so that any workgroup finds its segment by a search
 // over the offsets, with no list of them in memory; an example of one segment is written at once, the others' segments leave fp32
-// planes that a second kernel adds in their order.  Up to 64 examples a wavefront knows them all, and the workgroups are numbered from
+// planes that a second kernel adds in their order.  Up to 256 examples a wavefront knows them all, and the workgroups are numbered from
 // the longest segments to the shortest ones: none of the long ones begins last (32 ragged
-// examples of 16384 tokens, R = 128, D = 4096: 75 -> 56 us; 64 of 32768, R = 64: 77 -> 61).
+// examples of 16384 tokens, R = 128, D = 4096: 75 -> 56 us; 64 of 32768, R = 64: 77 -> 61; 128 of them: 86 -> 73).
 struct GradArgs {
     const void *dY; int64_t ldY;
     const int8_t *codes; int64_t ldC;
@@ -218,46 +218,73 @@ __device__ inline int64_t find_example(const GradArgs &a, int64_t j, int64_t chu
     }
     return (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)lo);
 }
-__device__ inline bool find_segment(const GradArgs &a, int64_t j, Segment &s) {
-    if (a.n <= 64) {                                       // example `lane`: `full` segments of a.chunk and one of `rest`
-        const int lane = threadIdx.x & 63, n = (int)a.n;
-        const int64_t o0 = offset_at(a, lane < n ? lane : n - 1), o1 = offset_at(a, lane < n ? lane + 1 : n), len = lane < n && o1 > o0 ? o1 - o0 : 0;
-        const int64_t full = len < a.chunk ? 0 : len / a.chunk, rest = len - full * a.chunk;
-        const bool ends = lane < n && (rest > 0 || full == 0);
-        int64_t upto = full;
-        if (__any(full > 0))
+// Up to 64 K examples, number 64 k + lane in `[k]` of a lane: `full` segments of a.chunk tokens each, and one of `rest` tokens, of which
+// the one with r longer ones (or as long and before it) is found by the bits of its length.
+template <int K> __device__ inline bool ranked_segment(const GradArgs &a, int64_t j, Segment &s) {
+    const int lane = threadIdx.x & 63, n = (int)a.n;
+    int64_t o0[K], o1[K], full[K], upto[K], fulls = 0;
+    int rest[K];                                           // -1: none
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int e = 64 * k + lane;
+        o0[k] = offset_at(a, e < n ? e : n);
+        o1[k] = offset_at(a, e < n ? e + 1 : n);
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int64_t len = o1[k] > o0[k] ? o1[k] - o0[k] : 0;
+        full[k] = len < a.chunk ? 0 : len / a.chunk;
+        upto[k] = full[k];
+        if (__any(full[k] > 0))
 #pragma unroll
             for (int d = 1; d < 64; d *= 2) {
-                const int64_t o = __shfl_up(upto, d, 64);
-                if (lane >= d) upto += o;
+                const int64_t o = __shfl_up(upto[k], d, 64);
+                if (lane >= d) upto[k] += o;
             }
-        const int64_t fulls = readlane64(upto, 63);
-        int at;
-        if (j < fulls) {
-            at = __ffsll((unsigned long long)__ballot(upto > j)) - 1;
-            s.lo = readlane64(o0, at) + (j - readlane64(upto - full, at)) * a.chunk;
-            s.hi = s.lo + a.chunk;
-        } else {
-            const int key = !ends ? -1 : rest < 0x7FFFFFFF ? (int)rest : 0x7FFFFFFF;
-            int longer = 0;
-            for (int i = 0; i < n; ++i) {
-                const int k = __builtin_amdgcn_readlane(key, i);
-                longer += k > key || (k == key && i < lane);
-            }
-            const uint64_t it = __ballot(ends && longer == j - fulls);
-            if (it == 0) return false;
-            at = __ffsll((unsigned long long)it) - 1;
-            s.hi = readlane64(o0 + len, at);
-            s.lo = s.hi - readlane64(rest, at);
-        }
-        s.lo = readlane64(s.lo, 0);                        // in scalar registers: bases of the copies
-        s.hi = readlane64(s.hi, 0);
-        s.e = at;
-        s.whole = readlane64(len, at) <= a.chunk;
-        const int64_t first = readlane64(o0, at);
-        s.plane = s.whole ? 0 : at + first / a.chunk + (s.lo - first) / a.chunk;
-        return true;
+        upto[k] += fulls;
+        fulls = readlane64(upto[k], 63);
+        const int64_t left = len - full[k] * a.chunk;
+        rest[k] = 64 * k + lane >= n || (left == 0 && len > 0) ? -1 : left < 0x3FFFFFFF ? (int)left : 0x3FFFFFFF;
     }
+    auto count = [&](int least) {
+        int c = 0;
+#pragma unroll
+        for (int k = 0; k < K; ++k) c += __popcll(__ballot(rest[k] >= least));
+        return c;
+    };
+    const bool whole_chunk = j < fulls;
+    int64_t r = j - fulls;
+    int length = 0;
+    if (!whole_chunk) {
+        if (r >= count(0)) return false;
+        for (int bit = a.chunk < 0x40000000 ? 1 << (31 - __clz((int)a.chunk)) : 0x20000000; bit > 0; bit >>= 1)
+            if (count(length | bit) > r) length |= bit;
+        r -= count(length + 1);
+    }
+    bool found = false;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        if (found) continue;
+        const uint64_t at_length = __ballot(rest[k] == length), it = __ballot(whole_chunk ? upto[k] > j : rest[k] == length && __popcll(at_length & (((uint64_t)1 << lane) - 1)) == r);
+        if (it == 0) {
+            r -= __popcll(at_length);
+            continue;
+        }
+        found = true;
+        const int at = __ffsll((unsigned long long)it) - 1;
+        const int64_t first = readlane64(o0[k], at), end = readlane64(o1[k], at), len = end > first ? end - first : 0, whole = readlane64(full[k], at);
+        const int64_t i = whole_chunk ? j - (readlane64(upto[k], at) - whole) : whole;
+        s.e = 64 * k + at;
+        s.lo = readlane64(first + i * a.chunk, 0);         // in scalar registers: bases of the copies
+        s.hi = readlane64(whole_chunk ? s.lo + a.chunk : first + len, 0);
+        s.whole = len <= a.chunk;
+        s.plane = s.whole ? 0 : s.e + first / a.chunk + i;
+    }
+    return found;
+}
+__device__ inline bool find_segment(const GradArgs &a, int64_t j, Segment &s) {
+    if (a.n <= 64) return ranked_segment<1>(a, j, s);
+    if (a.n <= 256) return ranked_segment<4>(a, j, s);
     int64_t o0, o1;
     s.e = find_example(a, j, a.chunk, o0, o1);
     if (s.e < 0) return false;

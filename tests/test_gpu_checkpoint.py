@@ -172,6 +172,30 @@ def test_weight_gradients(R, D, ends, pad, dtY, dtG):
     assert (wide[:, :5] == 7).all() and (wide[:, 5 + R * D:] == 7).all()
 
 
+@pytest.mark.parametrize("n", [2, 63, 64, 65, 128, 255, 256, 257, 600])
+@pytest.mark.parametrize("how", ["ragged", "alike", "one long"])
+@pytest.mark.parametrize("dtY", [torch.bfloat16, torch.float32])
+def test_many_examples(n, how, dtY):
+    """Examples of any lengths, in parts or whole, none of them lost and none taken twice, whatever the order of the work."""
+    _say("gradient of many examples n=%d %s %s" % (n, how, dtY))
+    g = torch.Generator().manual_seed(n)
+    if how == "ragged":
+        T = 9 * n + 1500
+        ends = [0] + torch.sort(torch.randint(0, T // 2, (n - 2,), generator=g)).values.tolist() + [T // 2, T]
+    elif how == "alike":
+        T = 7 * n
+        ends = list(range(0, T + 1, 7))
+    else:
+        T = 3000
+        ends = [0] * (n // 2 + 1) + [T] * (n - n // 2)
+    codes, steps = plain.checkpoint(_inputs(T, 144, n))
+    dY = (torch.randn(T, 8, generator=g) * 1e-3).to(dtY)
+    ref, size = plain.weight_gradients(dY, codes, steps, ends)
+    G = Q.checkpoint8_grad(dY.to(DEV), codes.to(torch.int8).to(DEV), steps.float().to(DEV), torch.tensor(ends, device=DEV))
+    assert ((G.cpu().double() - ref).abs() <= _bound(ends, size, ref, torch.float32)).all()
+
+
+
 def test_no_tokens_and_no_examples():
     _say("gradient of nothing")
     empty = (torch.empty(0, 4, device=DEV), torch.empty(0, 200, dtype=torch.int8, device=DEV), torch.empty(0, 2, device=DEV))
