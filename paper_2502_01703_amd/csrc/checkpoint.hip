@@ -432,21 +432,25 @@ checkpoint_grad_kernel(GradArgs a) {
     }
 }
 
-// The same for bfloat16 gradients and operands whose rows are whole 16-byte chunks (or were made so).  A workgroup takes RT rows of R x GROUPS groups, a
+// The same for operands whose rows are whole 16-byte chunks (or were made so).  A workgroup takes RT rows of R x GROUPS groups, a
 // wavefront of it one group (or half of one); stages of 32 tokens' codes, gradients and steps are copied to a ring of NS in LDS
-// without passing through registers, three of them on their way while one is used: codes stay 8 bits wide until the transposing
-// reads have brought eight tokens of a column into a lane, and the step is multiplied there, into the gradients or, from 33 rows on,
-// into the codes (either product has 16 bits: two bfloat16 numbers).  Bound: memory while R is a rank of adapters (codes are read once
-// for 128 rows); the vector work of a stage is 12 operations for eight numbers of one side and 40 for eight of the other.  64 x 512 tokens
-// of 4096 columns: 47 us at R = 16, 37 of them the copies and their start; R = 64: 78 us in halves of a group per wavefront
-// with the steps in the codes, 98 in whole groups with the steps in the gradients (and half the wavefronts' room in registers).
+// without passing through registers, the next ones on their way while one is used: codes stay 8 bits wide until the transposing
+// reads have brought eight tokens of a column into a lane, and the step is multiplied there, into the gradients or, for bfloat16 ones from 33
+// rows on, into the codes (either product has 16 bits: two bfloat16 numbers).  Bound: memory while R is a rank of adapters (codes are read once
+// for 128 rows); the vector work of a stage is 12 operations for eight numbers of one side and 40 for eight of the other (60 - 80 for
+// fp32 gradients).  64 examples of 32768 tokens, 4096 columns: 42 us at R = 16 (codes alone 26); R = 64: 62 us in halves of a group per wavefront
+// with the steps in the codes, a quarter more in whole groups with the steps in the gradients (and half the wavefronts' room in registers).
+// fp32 gradients are read as rows of twice as many 16-bit columns: a pair of lanes holds the halves of two rows of them (eight apart), and
+// exchanges two.  Their products with a step are rounded to fp32 and taken as three bfloat16 terms for fp32 results (all 24 bits), two for bfloat16 ones: R = 16, 64,
+// 128 (32 examples of 16384 tokens) 46, 90, 93 us, against 62, 121, 168 without the ring.
 // Rows of 128 codes are exchanged by 16-byte chunks, rows of gradients by 32-byte pieces, so that the eight (four) rows of each of two
 // lane groups lie in different banks.
-template <int RT> struct GradRing {
-    static constexpr int NW = 4, SPLIT = RT >= 32 ? 2 : 1, GROUPS = NW / SPLIT, KT = 32, NS = 4, CM = 8 / SPLIT, CN = RT / 16;     // SPLIT: wavefronts of a group
-    static constexpr int CODES = GROUPS * KT * 128, Y = KT * RT * 2, STAGE = CODES + Y + NW * 256, LDS = NS * STAGE;
-    static constexpr bool SCALE_CODES = RT >= 64;          // the side with fewer fragments takes the steps
-    static constexpr int UC = 4 / SPLIT, YQ = Y / 1024, UY = (YQ + NW - 1) / NW, U = UC + UY + 1;
+template <int RT, class Y> struct GradRing {
+    static constexpr bool F32 = sizeof(Y) == 4;
+    static constexpr int NW = 4, SPLIT = RT >= 32 ? 2 : 1, GROUPS = NW / SPLIT, KT = 32, NS = F32 && RT >= 128 ? 3 : 4, CM = 8 / SPLIT, CN = RT / 16;     // SPLIT: wavefronts of a group
+    static constexpr int ROW = RT * (int)sizeof(Y), CODES = GROUPS * KT * 128, YS = KT * ROW, STAGE = CODES + YS + NW * 256, LDS = NS * STAGE;
+    static constexpr bool SCALE_CODES = RT >= 64 && !F32;          // the side with fewer fragments takes the steps
+    static constexpr int UC = 4 / SPLIT, YQ = YS / 1024, UY = (YQ + NW - 1) / NW, U = UC + UY + 1;
     static_assert((NS - 2) * U < 64, "vmcnt is a 6-bit counter");
 };
 __device__ inline bf16x8 upper_halves(const float (&v)[8]) {
@@ -455,20 +459,23 @@ __device__ inline bf16x8 upper_halves(const float (&v)[8]) {
     for (int h = 0; h < 4; ++h) r.u[h] = __builtin_amdgcn_perm(__float_as_uint(v[2 * h + 1]), __float_as_uint(v[2 * h]), 0x07060302u);
     return r.b;
 }
-// Numbers of at most 16 significant bits as sums of two bfloat16: their upper halves, and the rest, which has eight bits.
-__device__ inline void two_terms(const float (&v)[8], bf16x8 &first, bf16x8 &second) {
-    float rest[8];
+// Numbers as sums of bfloat16, of eight significant bits each: two terms hold 16 bits, three all of an fp32 number.
+template <int TERMS> __device__ inline void in_terms(float (&v)[8], bf16x8 (&out)[TERMS]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) rest[i] = __fsub_rn(v[i], __uint_as_float(__float_as_uint(v[i]) & 0xFFFF0000u));
-    first = upper_halves(v);
-    second = upper_halves(rest);
+    for (int t = 0; t < TERMS; ++t) {
+        out[t] = upper_halves(v);
+        if (t + 1 < TERMS)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = __fsub_rn(v[i], __uint_as_float(__float_as_uint(v[i]) & 0xFFFF0000u));
+    }
 }
 
-template <int RT, class Out>
-__global__ void __launch_bounds__(64 * GradRing<RT>::NW, 2)
+template <int RT, class Y, class Out>
+__global__ void __launch_bounds__(256, 2)
 checkpoint_grad_ring_kernel(GradArgs a) {
-    typedef GradRing<RT> Sh;
-    constexpr int GROUPS = Sh::GROUPS, KT = Sh::KT, NS = Sh::NS, CM = Sh::CM, CN = Sh::CN, YL = RT / 8;      // YL: lanes of a row of gradients
+    typedef GradRing<RT, Y> Sh;
+    constexpr int GROUPS = Sh::GROUPS, KT = Sh::KT, NS = Sh::NS, CM = Sh::CM, CN = Sh::CN, ROW = Sh::ROW, YL = ROW / 16, YB = (int)sizeof(Y);      // YL: lanes of a row of gradients
+    constexpr int TERMS = Sh::F32 && sizeof(Out) == 4 ? 3 : 2;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int64_t tiles = (int64_t)a.rtiles * a.dtiles, j = blockIdx.x / tiles;
     const int tile = (int)(blockIdx.x - j * tiles), rt = tile / a.dtiles, gt = (tile - rt * a.dtiles) * GROUPS;
@@ -478,7 +485,7 @@ checkpoint_grad_ring_kernel(GradArgs a) {
     const unsigned lds0 = (unsigned)(uintptr_t)((__attribute__((address_space(3))) unsigned char *)smem);
     const int groups = (a.D + kGroup - 1) / kGroup, r0 = rt * RT;
     const int gl = wave / Sh::SPLIT, c0 = wave % Sh::SPLIT * 64, g = gt + gl < groups ? gt + gl : groups - 1;
-    auto yswizzle = [](int k) { return RT >= 128 ? k & 7 : RT == 64 ? (k >> 1) & 3 : RT == 32 ? (k >> 2) & 1 : 0; };
+    auto yswizzle = [](int k) { return ROW >= 256 ? k & 7 : ROW == 128 ? (k >> 1) & 3 : ROW == 64 ? (k >> 2) & 1 : 0; };
     auto swizzle = [](int k) { return ((k >> 1) & 3) | ((k >> 4) & 1) << 2; };
 
     // ---- copies: what lane and wavefront take of a stage; rows past the segment repeat its last one, bytes past a row's end its last chunk
@@ -496,16 +503,16 @@ checkpoint_grad_ring_kernel(GradArgs a) {
     for (int u = 0; u < Sh::UY; ++u) {
         const int q = wave * Sh::UY + u < Sh::YQ ? wave * Sh::UY + u : Sh::YQ - 1;
         yrow[u] = q * (64 / YL) + lane / YL;
-        const int at = r0 * 2 + ((lane % YL) ^ (yswizzle(yrow[u]) << 1)) * 16;
-        ycol[u] = (unsigned)(at < a.Rc * 2 - 16 ? at : a.Rc * 2 - 16);
+        const int at = r0 * YB + ((lane % YL) ^ (yswizzle(yrow[u]) << 1)) * 16;
+        ycol[u] = (unsigned)(at < a.Rc * YB - 16 ? at : a.Rc * YB - 16);
     }
-    const unsigned ldC = (unsigned)a.ldC, ldY = (unsigned)a.ldY * 2, ldS = (unsigned)a.ldS * 4;
+    const unsigned ldC = (unsigned)a.ldC, ldY = (unsigned)a.ldY * YB, ldS = (unsigned)a.ldS * 4;
     auto request = [&](int s, int slot) {
         if (s > stages - 1) s = stages - 1;                // repeated past the end: all stages count alike
         const int64_t t = seg.lo + (int64_t)s * KT;
         const int last = len - s * KT - 1;                 // row
         const unsigned at = lds0 + (unsigned)(slot * Sh::STAGE);
-        const unsigned char *c = (const unsigned char *)a.codes + t * a.ldC, *y = (const unsigned char *)a.dY + t * a.ldY * 2;
+        const unsigned char *c = (const unsigned char *)a.codes + t * a.ldC, *y = (const unsigned char *)a.dY + t * a.ldY * YB;
 #pragma unroll
         for (int u = 0; u < Sh::UC; ++u) global_to_lds16(c, (unsigned)(crow[u] < last ? crow[u] : last) * ldC + ccol[u], at + (unsigned)((wave * Sh::UC + u) * 1024));
 #pragma unroll
@@ -514,18 +521,21 @@ checkpoint_grad_ring_kernel(GradArgs a) {
             global_to_lds16(y, (unsigned)(yrow[u] < last ? yrow[u] : last) * ldY + ycol[u], at + (unsigned)(Sh::CODES + q * 1024));
         }
         const int row = lane & 31;
-        global_to_lds4(a.step + t * a.ldS + g, (unsigned)(row < last ? row : last) * ldS, at + (unsigned)(Sh::CODES + Sh::Y + wave * 256));
+        global_to_lds4(a.step + t * a.ldS + g, (unsigned)(row < last ? row : last) * ldS, at + (unsigned)(Sh::CODES + Sh::YS + wave * 256));
     };
 
     // ---- operands: a lane's eight tokens are 4 quad .. + 3 and 16 + 4 quad .. + 3
     const int krow = (l16 >> 1) < 4 ? 4 * quad + (l16 >> 1) : 12 + 4 * quad + (l16 >> 1);
     const unsigned c_lane = (unsigned)(gl * KT * 128 + krow * 128 + (((swizzle(krow) ^ (c0 >> 4)) << 4) | (l16 & 1) << 3));
     const int yk = 4 * quad + (l16 >> 2);
-    const unsigned y_lane = (unsigned)(Sh::CODES + yk * RT * 2 + (yswizzle(yk) << 5) + (l16 & 3) * 8);
-    const unsigned s_lane = (unsigned)(Sh::CODES + Sh::Y + wave * 256 + quad * 16);
+    const unsigned y_lane = (unsigned)(Sh::CODES + yk * ROW + (yswizzle(yk) << 5) + (l16 & 3) * 8);
+    const unsigned s_lane = (unsigned)(Sh::CODES + Sh::YS + wave * 256 + quad * 16);
     typedef __attribute__((address_space(3))) i16x4 lds16x4;
     typedef __attribute__((ext_vector_type(2))) int i32x2;
     typedef __attribute__((address_space(3))) i32x2 lds32x2;
+
+    typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+    const bool odd = lane & 1;
 
     f32x4 acc[CM][CN];
 #pragma unroll
@@ -555,55 +565,81 @@ checkpoint_grad_ring_kernel(GradArgs a) {
                     w[4 + i] = 16 + 4 * quad + i < left ? w[4 + i] : 0.0f;
                 }
             }
-            bf16x8 fy[2][CN];                              // (fy[1]: the second terms, if they are the gradients')
-#pragma unroll
-            for (int n = 0; n < CN; ++n) {
-                const unsigned char *p = st + (y_lane ^ (unsigned)(n << 5));
+            auto column = [&](int piece) {                 // eight tokens of one of 16 columns of 16 bits
+                const unsigned char *p = st + (y_lane ^ (unsigned)(piece << 5));
                 const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)p);
-                const i16x4 z = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)(p + 16 * RT * 2));
-                fy[0][n] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, z, 0, 1, 2, 3, 4, 5, 6, 7));
-                if (!Sh::SCALE_CODES) {
-                    float v[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = __fmul_rn((float)fy[0][n][i], w[i]);
-                    two_terms(v, fy[0][n], fy[1][n]);
-                }
-            }
-#pragma unroll
-            for (int m = 0; m < CM; ++m) {
+                const i16x4 z = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)(p + 16 * ROW));
+                return __builtin_shufflevector(x, z, 0, 1, 2, 3, 4, 5, 6, 7);
+            };
+            auto codes_of = [&](int m, float (&v)[8]) {
                 const i32x2 b = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds32x2 *)(st + (c_lane ^ (unsigned)(m << 4))));
-                float v[8];
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
                     const int x = b[h >> 1] >> (16 * (h & 1));
                     v[2 * h] = (float)(int8_t)x;
                     v[2 * h + 1] = (float)(int8_t)(x >> 8);
                 }
-                bf16x8 fc[2];
-                if (Sh::SCALE_CODES) {
+            };
+            float v[8];
+            if (Sh::SCALE_CODES) {
+                bf16x8 fy[CN], fc[2];
+#pragma unroll
+                for (int n = 0; n < CN; ++n) fy[n] = __builtin_bit_cast(bf16x8, column(n));
+#pragma unroll
+                for (int m = 0; m < CM; ++m) {
+                    codes_of(m, v);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], w[i]);
-                    two_terms(v, fc[0], fc[1]);
-                } else {
-                    fc[0] = upper_halves(v);
+                    in_terms(v, fc);
+#pragma unroll
+                    for (int term = 1; term >= 0; --term)
+#pragma unroll
+                        for (int n = 0; n < CN; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fc[term], fy[n], acc[m][n], 0, 0, 0);
+                }
+            } else {
+                bf16x8 fc[CM], fy[TERMS];
+#pragma unroll
+                for (int m = 0; m < CM; ++m) {
+                    codes_of(m, v);
+                    fc[m] = upper_halves(v);
                 }
 #pragma unroll
-                for (int term = 1; term >= 0; --term)
+                for (int n = 0; n < CN; ++n) {
+                    if (Sh::F32) {
+                        const u32x4 x = __builtin_bit_cast(u32x4, column(2 * n)), z = __builtin_bit_cast(u32x4, column(2 * n + 1));
 #pragma unroll
-                    for (int n = 0; n < CN; ++n)
-                        acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fc[Sh::SCALE_CODES ? term : 0], fy[Sh::SCALE_CODES ? 0 : term][n], acc[m][n], 0, 0, 0);
+                        for (int h = 0; h < 4; ++h) {
+                            const unsigned keep = odd ? z[h] : x[h], give = odd ? x[h] : z[h];
+                            const unsigned got = (unsigned)__builtin_amdgcn_update_dpp(0, (int)give, 0xB1, 0xF, 0xF, false);
+                            v[2 * h] = __uint_as_float(__builtin_amdgcn_perm(keep, got, odd ? 0x05040100u : 0x01000504u));
+                            v[2 * h + 1] = __uint_as_float(__builtin_amdgcn_perm(keep, got, odd ? 0x07060302u : 0x03020706u));
+                        }
+                    } else {
+                        const bf16x8 x = __builtin_bit_cast(bf16x8, column(n));
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] = (float)x[i];
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], w[i]);
+                    in_terms(v, fy);
+#pragma unroll
+                    for (int term = TERMS - 1; term >= 0; --term)
+#pragma unroll
+                        for (int m = 0; m < CM; ++m) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fc[m], fy[term], acc[m][n], 0, 0, 0);
+                }
             }
             slot = slot + 1 == NS ? 0 : slot + 1;
         }
         wait_vmcnt<0>();                                   // no copy is under way when the workgroup gives its LDS back
     }
     // a lane holds four columns of one row
+    const int l_row = Sh::F32 ? (l16 >> 1) + 8 * (l16 & 1) : l16;
     if (gt + gl >= groups) return;
     auto put = [&](auto *rows, auto tail) {                // rows of D columns
         typedef std::remove_pointer_t<decltype(rows)> E;
 #pragma unroll
         for (int n = 0; n < CN; ++n) {
-            const int r = r0 + n * 16 + l16;
+            const int r = r0 + n * 16 + l_row;
             if (r >= a.R) continue;
 #pragma unroll
             for (int m = 0; m < CM; ++m) {
@@ -765,11 +801,16 @@ static int64_t grad_chunk(int64_t T, int64_t n, int32_t R, int32_t D) {
     return (chunk + 63) / 64 * 64;
 }
 static size_t up16(size_t bytes) { return (bytes + 15) & ~(size_t)15; }
-// Rows that are no whole chunks are packed into the workspace, whatever they lie in: gradients first, then codes.
-static int32_t packed_R(int32_t R) { return (R + 7) / 8 * 8; }
+// Rows that are no whole chunks may be packed into the workspace, whatever they lie in: gradients first, then codes.  Both take a launch,
+// and codes as long as a product of 64 rows (32 x 32000 tokens, R = 100, D = 1333: 70 us packed, 127 read as they lie; 8 x 4000 tokens 33 and 31; 64 x 65536,
+// R = 16, D = 1001: 55 and 44; 16 x 16000, R = 6, D = 4096, gradients alone: 29 and 32).
+static bool worth_packing(int64_t T, int64_t n, int32_t R, int32_t D) { return T >= 20000000 / D || many_rows(T, n, R, D); }
+static int32_t packed_R(int32_t R, int bytes) { return (int32_t)up16((size_t)R * bytes) / bytes; }
 static int32_t packed_D(int32_t D) { return (D + 15) / 16 * 16; }
-static size_t packed_bytes(int64_t T, int32_t R, int32_t D) {
-    return (R % 8 ? (size_t)T * packed_R(R) * 2 : 0) + (D % 16 ? (size_t)T * packed_D(D) : 0);
+static size_t packed_bytes(int64_t T, int64_t n, int32_t R, int32_t D) {
+    if (!worth_packing(T, n, R, D)) return 0;
+    const size_t y2 = R % 8 ? (size_t)T * packed_R(R, 2) * 2 : 0, y4 = R % 4 ? (size_t)T * packed_R(R, 4) * 4 : 0;
+    return (y2 > y4 ? y2 : y4) + (D % 16 && R > 64 ? (size_t)T * packed_D(D) : 0);
 }
 static int64_t grad_segments(int64_t T, int64_t n, int64_t chunk) { return n + T / chunk; }
 
@@ -792,23 +833,24 @@ static qless_status launch_grad(GradArgs a, hipStream_t st) {
     launch_join<Out>(a, st);
     return launch_status();
 }
-template <int RT, class Out>
+template <int RT, class Y, class Out>
 static qless_status launch_ring(GradArgs a, hipStream_t st) {
-    QLESS_LDS_KERNEL((checkpoint_grad_ring_kernel<RT, Out>), GradRing<RT>::LDS);
+    typedef GradRing<RT, Y> Ring;
+    QLESS_LDS_KERNEL((checkpoint_grad_ring_kernel<RT, Y, Out>), Ring::LDS);
     a.rtiles = (a.R + RT - 1) / RT;
-    a.dtiles = (a.D + kGroup * GradRing<RT>::GROUPS - 1) / (kGroup * GradRing<RT>::GROUPS);
+    a.dtiles = (a.D + kGroup * Ring::GROUPS - 1) / (kGroup * Ring::GROUPS);
     const int64_t grid = a.segments * a.rtiles * a.dtiles;
     if (grid > 0x7FFFFFFF) return QLESS_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((checkpoint_grad_ring_kernel<RT, Out>), dim3((unsigned)grid), dim3(64 * GradRing<RT>::NW), GradRing<RT>::LDS, st, a);
+    hipLaunchKernelGGL((checkpoint_grad_ring_kernel<RT, Y, Out>), dim3((unsigned)grid), dim3(64 * Ring::NW), Ring::LDS, st, a);
     launch_join<Out>(a, st);
     return launch_status();
 }
-template <class Out>
+template <class Y, class Out>
 static qless_status launch_ring_rows(const GradArgs &a, hipStream_t st) {
-    if (a.R <= 16) return launch_ring<16, Out>(a, st);
-    if (a.R <= 32) return launch_ring<32, Out>(a, st);
-    if (a.R <= 64) return launch_ring<64, Out>(a, st);
-    return launch_ring<128, Out>(a, st);
+    if (a.R <= 16) return launch_ring<16, Y, Out>(a, st);
+    if (a.R <= 32) return launch_ring<32, Y, Out>(a, st);
+    if (a.R <= 64) return launch_ring<64, Y, Out>(a, st);
+    return launch_ring<128, Y, Out>(a, st);
 }
 template <class Y, int TERMS, class Out>
 static qless_status launch_grad_rows(const GradArgs &a, hipStream_t st) {
@@ -864,7 +906,7 @@ extern "C" size_t qless_checkpoint8_grad_workspace(int64_t T, int64_t n, int32_t
     if (T < 0 || n < 1 || R < 1 || D < 1) return 0;
     const int64_t segments = grad_segments(T, n, grad_chunk(T, n, R, D));
     const size_t planes = segments > n ? (size_t)segments * (size_t)R * (size_t)D * 4 : 0, rows = many_rows(T, n, R, D) ? expand_bytes(T, n, D, 2) : 0;
-    return up16((planes > rows ? planes : rows)) + packed_bytes(T, R, D);
+    return up16((planes > rows ? planes : rows)) + packed_bytes(T, n, R, D);
 }
 
 extern "C" qless_status qless_checkpoint8_grad(const void *dY, qless_dtype dtY, int64_t ldY, int32_t R, const int8_t *codes, int64_t ldC,
@@ -884,25 +926,28 @@ extern "C" qless_status qless_checkpoint8_grad(const void *dY, qless_dtype dtY, 
     const qless_status ready = device_ready();
     if (ready != QLESS_OK) return ready;
     const hipStream_t st = (hipStream_t)stream;
-    if (dtY == QLESS_BF16 && T > 0 && T <= 0x3FFFFFFF && (int64_t)T * (packed_R(R) / 8) < ((int64_t)1 << 38) && (int64_t)T * (packed_D(D) / 16) < ((int64_t)1 << 38)) {
-        unsigned char *pack = (unsigned char *)ws + (need - packed_bytes(T, R, D));
-        const bool many = expand_ld(D) < (1 << 22) && many_rows(T, n, R, D);
-        if (R % 8 != 0) {
-            a.Rc = packed_R(R);
-            launch_pack((const uint16_t *)dY, ldY, T, R, (uint16_t *)pack, a.Rc, st);
-            a.dY = pack; a.ldY = a.Rc;
-            pack += (size_t)T * a.Rc * 2;
+    const int bytes = dtY == QLESS_BF16 ? 2 : 4, rc = packed_R(R, bytes);
+    if (T > 0 && T <= 0x3FFFFFFF && (int64_t)T * (rc * (int64_t)bytes / 16) < ((int64_t)1 << 38) && (int64_t)T * (packed_D(D) / 16) < ((int64_t)1 << 38)) {
+        unsigned char *pack = (unsigned char *)ws + (need - packed_bytes(T, n, R, D));
+        const bool many = dtY == QLESS_BF16 && expand_ld(D) < (1 << 22) && many_rows(T, n, R, D);
+        if (rc != R && worth_packing(T, n, R, D)) {
+            if (bytes == 2) launch_pack((const uint16_t *)dY, ldY, T, R, (uint16_t *)pack, rc, st);
+            else launch_pack((const float *)dY, ldY, T, R, (float *)pack, rc, st);
+            a.dY = pack; a.ldY = a.Rc = rc;
+            pack += (size_t)T * rc * bytes;
         }
-        if (D % 16 != 0 && !many) {
+        if (D % 16 != 0 && R > 64 && !many && worth_packing(T, n, R, D)) {
             a.Dc = packed_D(D);
             launch_pack(codes, ldC, T, D, (int8_t *)pack, a.Dc, st);
             a.codes = (const int8_t *)pack; a.ldC = a.Dc;
         }
         // 16-byte copies and 32-bit offsets
-        const bool whole_y = (T == 1 || a.ldY % 8 == 0) && ((uintptr_t)a.dY & 15) == 0 && a.ldY < (1 << 22);
+        const bool whole_y = a.Rc == rc && (T == 1 || a.ldY * bytes % 16 == 0) && ((uintptr_t)a.dY & 15) == 0 && a.ldY < (1 << 22);
         if (whole_y && many) return dtG == QLESS_BF16 ? launch_many<1, uint16_t>(a, st) : launch_many<2, float>(a, st);
-        if (whole_y && (T == 1 || a.ldC % 16 == 0) && ((uintptr_t)a.codes & 15) == 0 && a.ldC < (1 << 24) && ldS < (1 << 24))
-            return dtG == QLESS_BF16 ? launch_ring_rows<uint16_t>(a, st) : launch_ring_rows<float>(a, st);
+        if (whole_y && a.Dc % 16 == 0 && (T == 1 || a.ldC % 16 == 0) && ((uintptr_t)a.codes & 15) == 0 && a.ldC < (1 << 24) && ldS < (1 << 24)) {
+            if (dtY == QLESS_BF16) return dtG == QLESS_BF16 ? launch_ring_rows<uint16_t, uint16_t>(a, st) : launch_ring_rows<uint16_t, float>(a, st);
+            return dtG == QLESS_BF16 ? launch_ring_rows<float, uint16_t>(a, st) : launch_ring_rows<float, float>(a, st);
+        }
     }
     if (dtY == QLESS_BF16) return dtG == QLESS_BF16 ? launch_grad_rows<uint16_t, 2, uint16_t>(a, st) : launch_grad_rows<uint16_t, 2, float>(a, st);
     return dtG == QLESS_BF16 ? launch_grad_rows<float, 2, uint16_t>(a, st) : launch_grad_rows<float, 3, float>(a, st);
