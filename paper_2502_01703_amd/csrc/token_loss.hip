@@ -43,7 +43,7 @@ struct LossTokens {                        // workspace views, by live token (pa
 };
 struct LossPlan {
     int64_t T, Tp, Dp, Vp, piece, parts;
-    int32_t D, V, tile_n, tile_m, splits, raw;
+    int32_t D, V, tile_n, tile_m, per_part, splits, raw;
     bool one_pass;                         // dW without a second pass
     size_t off[20], total;
 };
@@ -722,7 +722,6 @@ static LossPlan loss_plan(int64_t T, int32_t D, int32_t V, bool want_dH, bool wa
         p.raw = (int32_t)raw;
         p.tile_m = 256;
     }
-    p.parts = p.Vp / 32;                                    // at most (32 entries a part)
     p.one_pass = T <= kFew || (want_dW && p.Tp * p.Vp * 6 <= budget);
     const int64_t bytes = p.one_pass ? 6 : 2;               // of an entry of a piece
     int64_t piece = p.Vp;
@@ -736,6 +735,9 @@ static LossPlan loss_plan(int64_t T, int32_t D, int32_t V, bool want_dH, bool wa
         if (piece > p.Vp) piece = p.Vp;
     }
     p.piece = piece;
+    // (raw: its parts are larger.)  Where dH runs along powers of two the parts are a piece's
+    p.per_part = p.tile_m == 128 ? 64 : p.tile_n == 256 ? 128 : p.tile_n == 32 ? 32 : 64;
+    p.parts = (want_dH && !p.one_pass ? piece : p.Vp) / p.per_part;
     const int64_t tiles = ((D + 255) / 256) * ntiles, stages = piece / 64;
     int64_t splits = tiles > 0 ? cus / tiles : 1;
     if (splits > stages / 8) splits = stages / 8;
@@ -758,7 +760,7 @@ static LossPlan loss_plan(int64_t T, int32_t D, int32_t V, bool want_dH, bool wa
     take(whole > packed ? whole : packed);
     take(want_dH ? (size_t)p.splits * p.Tp * p.Dp * 4 : 0); // 16 planes
     take(p.raw > 1 ? (size_t)p.raw * p.Tp * p.Vp * 4 : 0);  // 17 raw
-    take(want_dH && T > kFew ? (size_t)(piece / 64) * p.Tp * 4 : 0);      // 18 shift
+    take(want_dH && T > kFew ? (size_t)(piece / p.per_part) * p.Tp * 4 : 0);      // 18 shift
     p.total = at;
     return p;
 }
@@ -788,7 +790,7 @@ static qless_status logits_product(const LossPlan &p, ProductArgs a, int64_t ent
 extern "C" size_t qless_token_loss_workspace(int64_t T, int32_t D, int32_t V, int want_dH, int want_dW) {
     using namespace qless;
     if (T < 0 || D < 1 || V < 1) return 0;
-    const size_t total = loss_plan(T, D, V, want_dH != 0, want_dW != 0).total, single = want_dH && !want_dW ? single_workspace(T, D, V) : 0;
+    const size_t total = loss_plan(T, D, V, want_dH != 0, want_dW != 0).total, single = want_dH ? single_workspace(T, D, V) : 0;
     return total > single ? total : single;
 }
 
@@ -797,7 +799,7 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
                                          void *dW, int64_t ldDW, void *ws, size_t ws_bytes, void *stream) {
     using namespace qless;
     if (T < 0 || D < 1 || V < 1 || (T > 1 && (ldH < D || (dH && ldDH < D))) || (V > 1 && (ldW < D || (dW && ldDW < D)))) return QLESS_ERR_INVALID_ARG;
-    if (dt != QLESS_BF16 || D > 65536 || T > 0x3FFFFFFF) return QLESS_ERR_UNSUPPORTED;
+    if (dt != QLESS_BF16 || D > 65536 || T > 0x3FFFFFFF || V > 0x3FFFFFFF) return QLESS_ERR_UNSUPPORTED;
     if (T == 0 && !dW) return QLESS_OK;
     if (!W || (T > 0 && (!H || !target || !nll))) return QLESS_ERR_INVALID_ARG;
     if (!ws || ws_bytes < qless_token_loss_workspace(T, D, V, dH != nullptr, dW != nullptr) || ((uintptr_t)ws & 15) != 0) return QLESS_ERR_WORKSPACE;
@@ -839,7 +841,7 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
     };
     const ProductOperand tokens{w.H, p.Dp * 2, p.Tp, p.Dp * 2};
     const bool raw = p.raw > 1 && piece == p.Vp;
-    const int per_part = raw ? kGather : p.tile_m == 128 ? 64 : p.tile_n == 256 ? 128 : p.tile_n == 32 ? 32 : 64;
+    const int per_part = raw ? kGather : p.per_part;
     auto parts_of = [&](int64_t entries) { return (entries + per_part - 1) / per_part; };
     auto hidden_product = [&](const ProductOperand &rows, int64_t n, int64_t v0) {        // dH's planes: rows m columns of W, columns n tokens
         const ProductArgs a{ProductOperand{rows.base, rows.ld, rows.depth, n}, ProductOperand{w.delta, piece * 2, few ? 2 * kFew : p.Tp, up_to(n, 64) * 2},

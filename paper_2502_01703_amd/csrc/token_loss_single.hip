@@ -242,8 +242,14 @@ bool single_serves(int64_t T, int32_t D, int32_t V) {
     if (T < 1 || T > 4 || D > 8192 || T * single_units(D) > 8) return false;
     return T <= 2 || (D > 2048 && D <= 4096) || (int64_t)V * D <= (4 << 20);
 }
+static int single_share(int32_t D, int32_t V) {            // rows of W of a workgroup: a batch at least
+    const int groups = single_groups(D), share = (V + groups - 1) / groups, batch = 8 / single_units(D);
+    return share < batch ? batch : share;
+}
+static int single_used(int32_t D, int32_t V) { return (V + single_share(D, V) - 1) / single_share(D, V); }       // workgroups that have rows
+static size_t single_parts(int64_t T, int32_t D, int32_t V) { return ((size_t)single_used(D, V) * T * 8 + 255) & ~(size_t)255; }
 size_t single_workspace(int64_t T, int32_t D, int32_t V) {
-    return single_serves(T, D, V) ? 256 + (size_t)single_groups(D) * T * 8 + (size_t)single_groups(D) * T * single_dp(D) * 4 : 0;
+    return single_serves(T, D, V) ? 256 + single_parts(T, D, V) + (size_t)single_used(D, V) * T * single_dp(D) * 4 : 0;
 }
 
 template <int TT, int KU, int NW>
@@ -254,13 +260,10 @@ static void launch_single_as(const SingleArgs &a, int groups, hipStream_t st) {
 
 qless_status launch_single(const uint16_t *H, int64_t ldH, const uint16_t *W, int64_t ldW, int T, int32_t D, int32_t V, const int64_t *target,
                            const float *weight, float *nll, float *lse, uint16_t *dH, int64_t ldDH, void *ws, hipStream_t st) {
-    const int groups = single_groups(D);
+    const int used = single_used(D, V), units = single_units(D);
     unsigned char *base = (unsigned char *)ws;
-    SingleArgs a{H, ldH, W, ldW, target, weight, T, D, V, (V + groups - 1) / groups, (float *)base, (float2 *)(base + 256),
-                 (float *)(base + 256 + (size_t)groups * T * 8), single_dp(D), nll, lse, dH, ldDH};
-    const int units = single_units(D);
-    if (a.share < 8 / units) a.share = 8 / units;           // a batch
-    const int used = (V + a.share - 1) / a.share;           // workgroups that have rows
+    SingleArgs a{H, ldH, W, ldW, target, weight, T, D, V, single_share(D, V), (float *)base, (float2 *)(base + 256),
+                 (float *)(base + 256 + single_parts(T, D, V)), single_dp(D), nll, lse, dH, ldDH};
     auto by_tokens = [&](auto ku, auto waves) {
         constexpr int KU = decltype(ku)::value, NW = decltype(waves)::value;
         if (T == 1) launch_single_as<1, KU, NW>(a, used, st);

@@ -31,3 +31,17 @@ def test_workspace_does_not_hold_the_logits():
     L = binding.lib()
     T, D, V = 65536, 4096, 131072
     assert L.qless_token_loss_workspace(T, D, V, 1, 1) < T * V * 2 // 4
+
+
+def test_vocabularies_that_32_bits_do_not_count_are_refused():
+    L = binding.lib()
+    for V in (1 << 30, (1 << 31) - 1):
+        for T in (1, 100):
+            assert L.qless_token_loss(one, 64, one, 64, 1, T, 64, V, one, None, one, None, one, 64, None, 0, one, 1 << 62, None) == UNSUPPORTED
+
+
+def test_a_workspace_for_more_outputs_serves_fewer():
+    L = binding.lib()
+    for T, D, V in ((1, 64, 100), (1, 4096, 32000), (2, 8192, 7), (4, 4096, 1000), (31, 100, 5000), (40, 8192, 4000), (300, 264, 3001), (9000, 40, 100000)):
+        loss, dH, dW, both = (L.qless_token_loss_workspace(T, D, V, *want) for want in ((0, 0), (1, 0), (0, 1), (1, 1)))
+        assert 0 < loss <= dH <= both and loss <= dW <= both
