@@ -297,25 +297,65 @@ __device__ inline bool find_segment(const GradArgs &a, int64_t j, Segment &s) {
     return true;
 }
 
+// What a wavefront writes: its accumulators (a lane holds four columns of one row) through LDS of its own, so that the lanes of a
+// store lie along rows of G (64 examples of 32768 tokens, R = 64, D = 4096: 61 -> 56 us; 2 of 11, R = 2409, D = 7603: 123 -> 86).  `row`: the lane's row of 16; first: of the tile.
+template <int CM, int CN, class E, bool TAIL>
+__device__ inline void put_tile(unsigned char *lds, const f32x4 (&acc)[CM][CN], E *out, int row, int r0, int d0, int32_t R, int32_t D) {
+    constexpr int LD = CM * 64 + 16, LANES = CM * 4;       // of a row
+    const int lane = threadIdx.x & 63, quad = lane >> 4, at = lane / LANES, c = lane % LANES * 4, left = D - d0 - c;
+    out += d0 + c;
+#pragma unroll
+    for (int n = 0; n < CN; ++n) {
+        __builtin_amdgcn_wave_barrier();                   // LDS operations of a wavefront complete in order
+#pragma unroll
+        for (int m = 0; m < CM; ++m) *(f32x4 *)(lds + row * LD + m * 64 + quad * 16) = acc[m][n];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < CM; ++i) {
+            const int k = i * (64 / LANES) + at, r = r0 + n * 16 + k;
+            const f32x4 y = *(const f32x4 *)(lds + k * LD + c * 4);
+            if (r >= R || left <= 0) continue;
+            E x[4], *to = out + (int64_t)r * D;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) x[u] = sizeof(E) == 2 ? (E)bf16_bits(y[u]) : (E)y[u];
+            if (!TAIL || left >= 4) __builtin_memcpy(to, x, sizeof x);
+            else
+#pragma unroll
+                for (int u = 0; u < 4; ++u) if (u < left) to[u] = x[u];
+        }
+    }
+}
+template <class Out, int CM, int CN>
+__device__ inline void put_segment(const GradArgs &a, const Segment &s, unsigned char *lds, const f32x4 (&acc)[CM][CN], int row, int r0, int d0) {
+    auto put = [&](auto tail) {
+        if (s.whole) put_tile<CM, CN, Out, decltype(tail)::value>(lds, acc, (Out *)a.G + s.e * a.ldG, row, r0, d0, a.R, a.D);
+        else put_tile<CM, CN, float, decltype(tail)::value>(lds, acc, a.planes + s.plane * a.R * (int64_t)a.D, row, r0, d0, a.R, a.D);
+    };
+    if (a.D % 4 == 0) put(std::false_type());              // (the code of partial stores is not fetched)
+    else put(std::true_type());
+}
+
 // Tiles of RT rows of R x 128 columns (one group: a token has one step there), four wavefronts, 64 tokens a stage.  A stage's codes
 // become bfloat16, its gradients times their step the sum of TERMS bfloat16; both lie in LDS as rows of a token, and the matrix operands
 // (eight tokens of a column in a lane) are formed by the transposing LDS reads.  The order of the tokens inside a product is that of
 // those reads, alike on both sides.  32-byte pieces of a row are exchanged by its token's low bits: the eight rows that 32 lanes read
-// together lie in different banks.
+// together lie in different banks.  RT is at most 64: with 128 rows one workgroup fits a compute unit, and waits for its loads alone (2 examples of 11 tokens,
+// R = 2409, D = 7603: 86 us, with 64 49; 8 of 4000 tokens, R = 100, D = 1333: 31 and 24).
 template <int RT, class Y, int TERMS, class Out>
 __global__ void __launch_bounds__(256)
 checkpoint_grad_kernel(GradArgs a) {
     constexpr int KT = 64, WY = RT >= 64 ? 2 : 1, WX = 4 / WY, CM = 128 / WX / 16, CN = RT / WY / 16;
     constexpr int YROW = RT * 2, YPLANE = KT * YROW, PIECES = KT * RT / 8, PER = (PIECES + 255) / 256;
-    __shared__ __attribute__((aligned(16))) unsigned char s_codes[KT * 256];
-    __shared__ __attribute__((aligned(16))) unsigned char s_y[TERMS * YPLANE];
+    __shared__ __attribute__((aligned(16))) unsigned char s_all[KT * 256 + TERMS * YPLANE];
+    unsigned char *s_codes = s_all, *s_y = s_all + KT * 256;
+    static_assert(16 * (CM * 64 + 16) * 4 <= KT * 256 + TERMS * YPLANE, "16 rows of each wavefront");
     const int64_t tiles = (int64_t)a.rtiles * a.dtiles, j = blockIdx.x / tiles;
     const int tile = (int)(blockIdx.x - j * tiles), rt = tile / a.dtiles, g = tile - rt * a.dtiles;
     Segment seg;
     if (!find_segment(a, j, seg)) return;                  // the whole workgroup
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wy = wave / WX, wx = wave % WX;
     const int r0 = rt * RT, d0 = g * kGroup, l16 = lane & 15, quad = lane >> 4;
-    auto yswizzle = [](int k) { return RT >= 128 ? k & 7 : RT == 64 ? (k >> 1) & 3 : RT == 32 ? (k >> 2) & 1 : 0; };
+    auto yswizzle = [](int k) { return RT == 64 ? (k >> 1) & 3 : RT == 32 ? (k >> 2) & 1 : 0; };
 
     f32x4 acc[CM][CN];
 #pragma unroll
@@ -409,27 +449,8 @@ checkpoint_grad_kernel(GradArgs a) {
                         acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fm[m], fn[term][n], acc[m][n], 0, 0, 0);
         }
     }
-    // a lane holds four columns of one row
-#pragma unroll
-    for (int n = 0; n < CN; ++n) {
-        const int r = r0 + (wy * CN + n) * 16 + l16;
-        if (r >= a.R) continue;
-#pragma unroll
-        for (int m = 0; m < CM; ++m) {
-            const int d = d0 + (wx * CM + m) * 16 + quad * 4, left = a.D - d;
-            if (left <= 0) continue;
-            if (!seg.whole) {
-                float *out = a.planes + (seg.plane * a.R + r) * (int64_t)a.D + d;
-                for (int i = 0; i < 4; ++i) if (i < left) out[i] = acc[m][n][i];
-            } else {
-                Out *out = (Out *)a.G + seg.e * a.ldG + (int64_t)r * a.D + d;
-                for (int i = 0; i < 4; ++i)
-                    if (i < left) {
-                        if (sizeof(Out) == 2) out[i] = (Out)bf16_bits(acc[m][n][i]); else out[i] = (Out)acc[m][n][i];
-                    }
-            }
-        }
-    }
+    __syncthreads();                                       // everyone has read the last stage
+    put_segment<Out>(a, seg, s_all + wave * 16 * (CM * 64 + 16), acc, l16, r0 + wy * CN * 16, d0 + wx * CM * 16);
 }
 
 // The same for operands whose rows are whole 16-byte chunks (or were made so).  A workgroup takes RT rows of R x GROUPS groups, a
@@ -437,17 +458,17 @@ checkpoint_grad_kernel(GradArgs a) {
 // without passing through registers, the next ones on their way while one is used: codes stay 8 bits wide until the transposing
 // reads have brought eight tokens of a column into a lane, and the step is multiplied there, into the gradients or, for bfloat16 ones from 33
 // rows on, into the codes (either product has 16 bits: two bfloat16 numbers).  Bound: memory while R is a rank of adapters (codes are read once
-// for 128 rows); the vector work of a stage is 12 operations for eight numbers of one side and 40 for eight of the other (60 - 80 for
-// fp32 gradients).  64 examples of 32768 tokens, 4096 columns: 42 us at R = 16 (codes alone 26); R = 64: 62 us in halves of a group per wavefront
+// for 128 rows, 64 of fp32); the vector work of a stage is 12 operations for eight numbers of one side and 40 for eight of the other (60 - 80 for
+// fp32 gradients).  64 examples of 32768 tokens, 4096 columns: 42 us at R = 16 (codes alone 26); R = 64: 56 us in halves of a group per wavefront
 // with the steps in the codes, a quarter more in whole groups with the steps in the gradients (and half the wavefronts' room in registers).
 // fp32 gradients are read as rows of twice as many 16-bit columns: a pair of lanes holds the halves of two rows of them (eight apart), and
 // exchanges two.  Their products with a step are rounded to fp32 and taken as three bfloat16 terms for fp32 results (all 24 bits), two for bfloat16 ones: R = 16, 64,
-// 128 (32 examples of 16384 tokens) 46, 90, 93 us, against 62, 121, 168 without the ring.
+// 128 (32 examples of 16384 tokens) 46, 89, 89 us, against 62, 99, 96 without the ring.
 // Rows of 128 codes are exchanged by 16-byte chunks, rows of gradients by 32-byte pieces, so that the eight (four) rows of each of two
 // lane groups lie in different banks.
 template <int RT, class Y> struct GradRing {
     static constexpr bool F32 = sizeof(Y) == 4;
-    static constexpr int NW = 4, SPLIT = RT >= 32 ? 2 : 1, GROUPS = NW / SPLIT, KT = 32, NS = F32 && RT >= 128 ? 3 : 4, CM = 8 / SPLIT, CN = RT / 16;     // SPLIT: wavefronts of a group
+    static constexpr int NW = 4, SPLIT = RT >= 32 ? 2 : 1, GROUPS = NW / SPLIT, KT = 32, NS = 4, CM = 8 / SPLIT, CN = RT / 16;     // SPLIT: wavefronts of a group
     static constexpr int ROW = RT * (int)sizeof(Y), CODES = GROUPS * KT * 128, YS = KT * ROW, STAGE = CODES + YS + NW * 256, LDS = NS * STAGE;
     static constexpr bool SCALE_CODES = RT >= 64 && !F32;          // the side with fewer fragments takes the steps
     static constexpr int UC = 4 / SPLIT, YQ = YS / 1024, UY = (YQ + NW - 1) / NW, U = UC + UY + 1;
@@ -632,35 +653,9 @@ checkpoint_grad_ring_kernel(GradArgs a) {
         }
         wait_vmcnt<0>();                                   // no copy is under way when the workgroup gives its LDS back
     }
-    // a lane holds four columns of one row
-    const int l_row = Sh::F32 ? (l16 >> 1) + 8 * (l16 & 1) : l16;
+    __syncthreads();                                       // everyone has read the last stage
     if (gt + gl >= groups) return;
-    auto put = [&](auto *rows, auto tail) {                // rows of D columns
-        typedef std::remove_pointer_t<decltype(rows)> E;
-#pragma unroll
-        for (int n = 0; n < CN; ++n) {
-            const int r = r0 + n * 16 + l_row;
-            if (r >= a.R) continue;
-#pragma unroll
-            for (int m = 0; m < CM; ++m) {
-                const int d = g * kGroup + c0 + m * 16 + quad * 4, left = a.D - d;
-                if (left <= 0) continue;
-                E x[4], *out = rows + (int64_t)r * a.D + d;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = sizeof(E) == 2 ? (E)bf16_bits(acc[m][n][i]) : (E)acc[m][n][i];
-                if (!tail || left >= 4) __builtin_memcpy(out, x, sizeof x);
-                else
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) if (i < left) out[i] = x[i];
-            }
-        }
-    };
-    auto put_all = [&](auto tail) {
-        if (seg.whole) put((Out *)a.G + seg.e * a.ldG, tail);
-        else put(a.planes + seg.plane * a.R * (int64_t)a.D, tail);
-    };
-    if (a.D % 4 == 0) put_all(std::false_type());          // (the code of partial stores is not fetched)
-    else put_all(std::true_type());
+    put_segment<Out>(a, seg, smem + wave * 16 * (CM * 64 + 16), acc, Sh::F32 ? (l16 >> 1) + 8 * (l16 & 1) : l16, r0, g * kGroup + c0);
 }
 
 // Rows of `cols` elements copied to rows of ld (whole 16-byte chunks) with zeros behind them, a chunk a thread.
@@ -802,15 +797,17 @@ static int64_t grad_chunk(int64_t T, int64_t n, int32_t R, int32_t D) {
 }
 static size_t up16(size_t bytes) { return (bytes + 15) & ~(size_t)15; }
 // Rows that are no whole chunks may be packed into the workspace, whatever they lie in: gradients first, then codes.  Both take a launch,
-// and codes as long as a product of 64 rows (32 x 32000 tokens, R = 100, D = 1333: 70 us packed, 127 read as they lie; 8 x 4000 tokens 33 and 31; 64 x 65536,
-// R = 16, D = 1001: 55 and 44; 16 x 16000, R = 6, D = 4096, gradients alone: 29 and 32).
+// and codes as long as a product of 64 rows, so that they are packed for more rows only, and where fp32 gradients do not make the vector work the
+// bound (R = 100, bfloat16: 64 x 65536 tokens, D = 4095 288 us packed, 394 read as they lie; 32 x 32000, D = 1333 65 and 74; 8 x 4000 33 and 31.  fp32 gradients, 32 x 32000: 91 and
+// 76.  R = 16, 64 x 65536, D = 1001: 55 and 44.  Gradients alone, D = 4096: 64 x 65536, R = 100 160 and 326; 16 x 16000, R = 6
+// 28 and 31; 16 x 4000 18.5 and 17.5).
 static bool worth_packing(int64_t T, int64_t n, int32_t R, int32_t D) { return T >= 20000000 / D || many_rows(T, n, R, D); }
 static int32_t packed_R(int32_t R, int bytes) { return (int32_t)up16((size_t)R * bytes) / bytes; }
 static int32_t packed_D(int32_t D) { return (D + 15) / 16 * 16; }
 static size_t packed_bytes(int64_t T, int64_t n, int32_t R, int32_t D) {
     if (!worth_packing(T, n, R, D)) return 0;
     const size_t y2 = R % 8 ? (size_t)T * packed_R(R, 2) * 2 : 0, y4 = R % 4 ? (size_t)T * packed_R(R, 4) * 4 : 0;
-    return (y2 > y4 ? y2 : y4) + (D % 16 && R > 64 ? (size_t)T * packed_D(D) : 0);
+    return (y2 > y4 ? y2 : y4) + (D % 16 && R > 64 ? (size_t)T * packed_D(D) : 0);      // (codes for bfloat16 gradients only)
 }
 static int64_t grad_segments(int64_t T, int64_t n, int64_t chunk) { return n + T / chunk; }
 
@@ -850,14 +847,14 @@ static qless_status launch_ring_rows(const GradArgs &a, hipStream_t st) {
     if (a.R <= 16) return launch_ring<16, Y, Out>(a, st);
     if (a.R <= 32) return launch_ring<32, Y, Out>(a, st);
     if (a.R <= 64) return launch_ring<64, Y, Out>(a, st);
-    return launch_ring<128, Y, Out>(a, st);
+    if constexpr (sizeof(Y) == 4) return launch_ring<64, Y, Out>(a, st);      // (R = 256, D = 2048: 158 us, with 128 rows 166)
+    else return launch_ring<128, Y, Out>(a, st);
 }
 template <class Y, int TERMS, class Out>
 static qless_status launch_grad_rows(const GradArgs &a, hipStream_t st) {
     if (a.R <= 16) return launch_grad<16, Y, TERMS, Out>(a, st);
     if (a.R <= 32) return launch_grad<32, Y, TERMS, Out>(a, st);
-    if (a.R <= 64) return launch_grad<64, Y, TERMS, Out>(a, st);
-    return launch_grad<128, Y, TERMS, Out>(a, st);
+    return launch_grad<64, Y, TERMS, Out>(a, st);
 }
 
 static bool checkpoint_shape_ok(int64_t T, int32_t D, int64_t ldX, int64_t ldC, int64_t ldS) {
@@ -936,7 +933,7 @@ extern "C" qless_status qless_checkpoint8_grad(const void *dY, qless_dtype dtY, 
             a.dY = pack; a.ldY = a.Rc = rc;
             pack += (size_t)T * rc * bytes;
         }
-        if (D % 16 != 0 && R > 64 && !many && worth_packing(T, n, R, D)) {
+        if (dtY == QLESS_BF16 && D % 16 != 0 && R > 64 && !many && worth_packing(T, n, R, D)) {
             a.Dc = packed_D(D);
             launch_pack(codes, ldC, T, D, (int8_t *)pack, a.Dc, st);
             a.codes = (const int8_t *)pack; a.ldC = a.Dc;
