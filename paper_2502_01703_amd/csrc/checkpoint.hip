@@ -687,8 +687,9 @@ static void launch_pack(const T *in, int64_t ld_in, int64_t rows, int32_t cols, 
 template <class Out, int W>
 __global__ void __launch_bounds__(256)
 checkpoint_join_kernel(GradArgs a) {
-    const int64_t e = blockIdx.y, size = (int64_t)a.R * a.D, p0 = phi(a, e, a.chunk), length = offset_at(a, e + 1) - offset_at(a, e);
+    const int64_t e = blockIdx.y, size = (int64_t)a.R * a.D, length = offset_at(a, e + 1) - offset_at(a, e);
     if (length <= a.chunk) return;
+    const int64_t p0 = phi(a, e, a.chunk);
     int64_t p1 = p0 + (length + a.chunk - 1) / a.chunk;
     if (p1 > a.segments) p1 = a.segments;
     typedef __attribute__((ext_vector_type(W))) float fw;
@@ -816,7 +817,8 @@ static void launch_join(const GradArgs &a, hipStream_t st) {
     if (a.segments <= a.n) return;
     const int64_t size = (int64_t)a.R * a.D;
     int64_t bx = (size + 1023) / 1024;
-    if (bx > 1024) bx = 1024;
+    const int64_t most = a.n <= 8 ? 1024 : a.n < 64 ? 8192 / a.n : 128;   // few of many examples have parts
+    if (bx > most) bx = most;
     if (size % 4 == 0) hipLaunchKernelGGL((checkpoint_join_kernel<Out, 4>), dim3((unsigned)bx, (unsigned)a.n), dim3(256), 0, st, a);
     else hipLaunchKernelGGL((checkpoint_join_kernel<Out, 1>), dim3((unsigned)bx, (unsigned)a.n), dim3(256), 0, st, a);
 }
