@@ -51,6 +51,7 @@ struct LossPlan {
 constexpr int kGather = 1024;              // entries of a part where partial logits are added
 constexpr int kFew = 32;                   // tokens up to which the rest of delta is two terms: rows t and t + kFew of delta and H
 
+constexpr int64_t kMostEntries = 1 << 22;  // of a piece: 32-bit offsets into a tile's rows of delta
 constexpr int kLossThreads = 1024;
 
 // The live tokens numbered in their order: a workgroup a thousand tokens, whose place follows from a count of the targets before them.
@@ -734,6 +735,7 @@ static LossPlan loss_plan(int64_t T, int32_t D, int32_t V, bool want_dH, bool wa
         piece = m * 256;
         if (piece > p.Vp) piece = p.Vp;
     }
+    if (piece > kMostEntries) piece = kMostEntries;
     p.piece = piece;
     // (raw: its parts are larger.)  Where dH runs along powers of two the parts are a piece's
     p.per_part = p.tile_m == 128 ? 64 : p.tile_n == 256 ? 128 : p.tile_n == 32 ? 32 : 64;
@@ -789,7 +791,7 @@ static qless_status logits_product(const LossPlan &p, ProductArgs a, int64_t ent
 
 extern "C" size_t qless_token_loss_workspace(int64_t T, int32_t D, int32_t V, int want_dH, int want_dW) {
     using namespace qless;
-    if (T < 0 || D < 1 || V < 1) return 0;
+    if (T < 0 || D < 1 || V < 1 || D > 65536 || T > 0x3FFFFFFF || V > 0x1FFFFFFF) return 0;
     const size_t total = loss_plan(T, D, V, want_dH != 0, want_dW != 0).total, single = want_dH ? single_workspace(T, D, V) : 0;
     return total > single ? total : single;
 }
@@ -799,7 +801,7 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
                                          void *dW, int64_t ldDW, void *ws, size_t ws_bytes, void *stream) {
     using namespace qless;
     if (T < 0 || D < 1 || V < 1 || (T > 1 && (ldH < D || (dH && ldDH < D))) || (V > 1 && (ldW < D || (dW && ldDW < D)))) return QLESS_ERR_INVALID_ARG;
-    if (dt != QLESS_BF16 || D > 65536 || T > 0x3FFFFFFF || V > 0x3FFFFFFF) return QLESS_ERR_UNSUPPORTED;
+    if (dt != QLESS_BF16 || D > 65536 || T > 0x3FFFFFFF || V > 0x1FFFFFFF) return QLESS_ERR_UNSUPPORTED;
     if (T == 0 && !dW) return QLESS_OK;
     if (!W || (T > 0 && (!H || !target || !nll))) return QLESS_ERR_INVALID_ARG;
     if (!ws || ws_bytes < qless_token_loss_workspace(T, D, V, dH != nullptr, dW != nullptr) || ((uintptr_t)ws & 15) != 0) return QLESS_ERR_WORKSPACE;

@@ -148,6 +148,16 @@ def test_pieces_read_in_place(want_dW):
     _check(H, W, y, w, Q.token_loss(H, W, y, w, want_dW=want_dW))
 
 
+@pytest.mark.parametrize("T,D,V", [(3, 16, 5000000), (40, 8, 5000000), (20, 12, 4300000)])
+def test_millions_of_entries(T, D, V):
+    """Rows of delta longer than 32-bit offsets reach over a tile: several pieces, also for few tokens."""
+    _say("loss of millions of entries T=%d D=%d V=%d" % (T, D, V))
+    H, W, y, w = _inputs(T, D, V, 13, masked=0.0)
+    y[0], y[1] = 0, V - 1
+    _check(H, W, y, w, Q.token_loss(H, W, y, w, want_dW=True))
+    _check(H, W, y, w, Q.token_loss(H, W, y, w))
+
+
 @pytest.mark.parametrize("T,D,V", [(130, 256, 1000), (700, 128, 9000), (9000, 40, 100000)])
 @pytest.mark.parametrize("rise", [-1.0, 1.0])
 def test_logits_that_rise_over_the_vocabulary(T, D, V, rise):
