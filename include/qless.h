@@ -333,8 +333,8 @@ qless_status qless_score_groups(const void *const *train_codes, const float *con
  *   target     device, T int64           weight   device, T fp32 (the inverse of an example's count of targets, say), or NULL: 1
  *   nll        device, T fp32            lse      device, T fp32, or NULL
  *   dH, dW     either or both may be NULL; both are written whole, not added to
- *   ws         device workspace, 16-byte aligned, of at least qless_token_loss_workspace(T, D, V, want_dH, want_dW) bytes; want_dH,
- *              want_dW: non-zero if dH (dW) is asked for
+ *   ws         device workspace, 16-byte aligned, of at least qless_token_loss_workspace(T, D, V, want_dH, want_dW) bytes (0 for sizes that are
+ *              refused); want_dH, want_dW: non-zero if dH (dW) is asked for
  * Arithmetic: products of bfloat16 are exact, logits, maxima, sums and losses fp32.  In the gradients a target's entry of
  * weight (softmax - onehot) is fp32, the others are rounded to bfloat16 once (up to 32 tokens: to two bfloat16 terms); sums are fp32 and
  * rounded once.  Results are run-to-run identical.  Rows of W and H
@@ -379,7 +379,8 @@ qless_status qless_checkpoint8_read(const int8_t *codes, int64_t ldC, const floa
  *   G        device, n rows of R * D, leading dimension ldG >= R * D (not read where n == 1), dtype dtG; what lies between the rows stays
  *   ws       device workspace, 16-byte aligned, of at least qless_checkpoint8_grad_workspace(T, n, R, D) bytes
  * Arithmetic: fp32 G: products of dY and step enter whole (dtY bfloat16) or to 2^-24 (fp32), products with codes are exact, sums are fp32.
- * bfloat16 G: dY * step is rounded to bfloat16 once, sums are fp32 and rounded once.  Results are run-to-run identical.
+ * bfloat16 G: one factor of a term (an activation, or dY * step) may be rounded to bfloat16 once (dY fp32: to 16 bits or more), sums are fp32 and rounded once.
+ * Results are run-to-run identical.
  * ------------------------------------------------------------------------------------------- */
 size_t qless_checkpoint8_grad_workspace(int64_t T, int64_t n, int32_t R, int32_t D);
 qless_status qless_checkpoint8_grad(const void *dY, qless_dtype dtY, int64_t ldY, int32_t R, const int8_t *codes, int64_t ldC,
