@@ -161,18 +161,20 @@ loss_single_kernel(SingleArgs a) {
     }
 }
 
-// Grid (tokens, 64 columns): the workgroups' parts of a token joined, four columns a thread, 16 threads sharing the planes.
+// Grid (tokens, 16 columns): the workgroups' parts of a token joined, four columns a thread, 64 threads sharing the planes, the first of which are
+// requested before the parts are (1 x 2048 x 32000: 5.6 us; with 16 threads, and none ahead, 8.3).
 __global__ void __launch_bounds__(256)
 loss_single_join_kernel(SingleArgs a, int groups) {
     __shared__ float s_top[4], s_sum[4], s_factor[kSingleGroups];
-    __shared__ float4 s_acc[256];
-    const int tid = threadIdx.x, t = blockIdx.x;
+    __shared__ float4 s_acc[16];
+    constexpr int AHEAD = 8;
+    const int tid = threadIdx.x, t = blockIdx.x, sub = tid >> 2;
     const int64_t y = a.target[t];
     const bool live = y >= 0 && y < a.V;
-    const int c = (int)blockIdx.y * 64 + (tid & 15) * 4;
+    const int c = (int)blockIdx.y * 16 + (tid & 3) * 4;
     uint16_t *out = a.dH + t * a.ldDH + c;
     if (!live) {
-        if (tid < 16)
+        if (tid < 4)
 #pragma unroll
             for (int u = 0; u < 4; ++u) if (c + u < a.D) out[u] = 0;
         if (tid == 0 && blockIdx.y == 0) {
@@ -181,9 +183,18 @@ loss_single_join_kernel(SingleArgs a, int groups) {
         }
         return;
     }
+    const bool on = c < a.D;                               // D is a multiple of eight
+    auto plane = [&](int g) { return on && g < groups ? *(const float4 *)(a.planes + ((int64_t)g * a.T + t) * a.Dp + c) : make_float4(0.0f, 0.0f, 0.0f, 0.0f); };
+    float4 ahead[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) ahead[i] = plane(sub + 64 * i);
+    uint16_t of_target[4] = {0, 0, 0, 0};
+    if (on) __builtin_memcpy(of_target, __builtin_assume_aligned(a.W + y * a.ldW + c, 8), 8);
+    const float hit = a.hit[t], w = a.weight ? a.weight[t] : 1.0f;
     float top = -INFINITY, sum = 0.0f;
     for (int g = tid; g < groups; g += 256) {
         const float2 x = a.part[(int64_t)g * a.T + t];
+        s_factor[g] = x.x;
         join_pair(top, sum, x.x, x.y);
     }
 #pragma unroll
@@ -197,35 +208,39 @@ loss_single_join_kernel(SingleArgs a, int groups) {
 #pragma unroll
     for (int i = 1; i < 4; ++i) join_pair(top, sum, s_top[i], s_sum[i]);
     const float ref = top == -INFINITY ? 0.0f : top;
-    for (int g = tid; g < groups; g += 256) s_factor[g] = __expf(a.part[(int64_t)g * a.T + t].x - ref);
+    for (int g = tid; g < groups; g += 256) s_factor[g] = __expf(s_factor[g] - ref);
     __syncthreads();
     float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (c < a.D) {                                          // D is a multiple of eight
-#pragma unroll 4
-        for (int g = tid >> 4; g < groups; g += 16) {
-            const float4 x = *(const float4 *)(a.planes + ((int64_t)g * a.T + t) * a.Dp + c);
-            const float f = s_factor[g];
-            s.x = __builtin_fmaf(f, x.x, s.x); s.y = __builtin_fmaf(f, x.y, s.y); s.z = __builtin_fmaf(f, x.z, s.z); s.w = __builtin_fmaf(f, x.w, s.w);
-        }
-    }
-    s_acc[tid] = s;
-    __syncthreads();
-    if (tid >= 16) return;
+    auto add = [&](float f, const float4 &x) {
+        s.x = __builtin_fmaf(f, x.x, s.x); s.y = __builtin_fmaf(f, x.y, s.y); s.z = __builtin_fmaf(f, x.z, s.z); s.w = __builtin_fmaf(f, x.w, s.w);
+    };
 #pragma unroll
-    for (int g = 1; g < 16; ++g) {
-        const float4 x = s_acc[g * 16 + tid];
+    for (int i = 0; i < AHEAD; ++i)
+        if (sub + 64 * i < groups) add(s_factor[sub + 64 * i], ahead[i]);
+#pragma unroll 4
+    for (int g = sub + 64 * AHEAD; g < groups; g += 64) add(s_factor[g], plane(g));
+#pragma unroll
+    for (int d = 4; d < 64; d *= 2) {
+        s.x += __shfl_xor(s.x, d, 64); s.y += __shfl_xor(s.y, d, 64); s.z += __shfl_xor(s.z, d, 64); s.w += __shfl_xor(s.w, d, 64);
+    }
+    if ((tid & 63) < 4) s_acc[(tid >> 6) * 4 + (tid & 3)] = s;
+    __syncthreads();
+    if (tid >= 4) return;
+#pragma unroll
+    for (int g = 1; g < 4; ++g) {
+        const float4 x = s_acc[g * 4 + tid];
         s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
     }
-    const float one = loss_of(top, sum, a.hit[t]), w = a.weight ? a.weight[t] : 1.0f, scale = w / sum, pull = w * expm1f(-one);
+    const float one = loss_of(top, sum, hit), scale = w / sum, pull = w * expm1f(-one);
     if (tid == 0 && blockIdx.y == 0) {
         a.nll[t] = one;
         if (a.lse) a.lse[t] = top + logf(sum);
     }
-    if (c >= a.D) return;
+    if (!on) return;
     const float f[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-        out[u] = __builtin_bit_cast(uint16_t, (__bf16)__builtin_fmaf(pull, low_half(a.W[y * a.ldW + c + u]), scale * f[u]));
+        out[u] = __builtin_bit_cast(uint16_t, (__bf16)__builtin_fmaf(pull, low_half(of_target[u]), scale * f[u]));
 }
 
 static int64_t single_dp(int32_t D) { return ((int64_t)D + 7) / 8 * 8; }
@@ -255,7 +270,7 @@ size_t single_workspace(int64_t T, int32_t D, int32_t V) {
 template <int TT, int KU, int NW>
 static void launch_single_as(const SingleArgs &a, int groups, hipStream_t st) {
     hipLaunchKernelGGL((loss_single_kernel<TT, KU, NW>), dim3((unsigned)groups), dim3(64 * NW), 0, st, a);
-    hipLaunchKernelGGL(loss_single_join_kernel, dim3((unsigned)a.T, (unsigned)((a.D + 63) / 64)), dim3(256), 0, st, a, groups);
+    hipLaunchKernelGGL(loss_single_join_kernel, dim3((unsigned)a.T, (unsigned)((a.D + 15) / 16)), dim3(256), 0, st, a, groups);
 }
 
 qless_status launch_single(const uint16_t *H, int64_t ldH, const uint16_t *W, int64_t ldW, int T, int32_t D, int32_t V, const int64_t *target,
