@@ -369,22 +369,27 @@ struct LossHead {
         const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
         const int block = __builtin_amdgcn_readfirstlane((int)((a.first + n) / 64));
         const int lo = a.start[block], hi = a.start[block + 1];
-        for (int x = lo; x < hi; ++x) {                    // in the order of target and token
-            const int r = __builtin_amdgcn_readfirstlane(a.order[x]), col = __builtin_amdgcn_readfirstlane(a.order_target[x]) & 63;
-            const float f = l32 == (col & 31) ? a.pull[r] : 0.0f;
-            const uint16_t *h = a.H + r * a.Dp + m + 4 * half;
-            auto add = [&](int j) {
+        for (int x0 = lo; x0 < hi; x0 += 64) {             // in the order of target and token; 64 of them in the lanes
+            const bool on = x0 + lane < hi;
+            const int rows = on ? a.order[x0 + lane] : 0, cols = on ? a.order_target[x0 + lane] & 63 : 0;
+            const float pulls = on ? a.pull[rows] : 0.0f;
+            for (int x = 0; x < 64 && x0 + x < hi; ++x) {
+                const int r = __builtin_amdgcn_readlane(rows, x), col = __builtin_amdgcn_readlane(cols, x);
+                const float pull = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(pulls), x)), f = l32 == (col & 31) ? pull : 0.0f;
+                const uint16_t *h = a.H + r * a.Dp + m + 4 * half;
+                auto add = [&](int j) {
 #pragma unroll
-                for (int i = 0; i < FM; ++i)
+                    for (int i = 0; i < FM; ++i)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        uint16_t y[4] = {0, 0, 0, 0};
-                        if (m + 32 * i + 8 * q + 4 * half < a.Dp) __builtin_memcpy(y, __builtin_assume_aligned(h + 32 * i + 8 * q, 8), 8);
+                        for (int q = 0; q < 4; ++q) {
+                            uint16_t y[4] = {0, 0, 0, 0};
+                            if (m + 32 * i + 8 * q + 4 * half < a.Dp) __builtin_memcpy(y, __builtin_assume_aligned(h + 32 * i + 8 * q, 8), 8);
 #pragma unroll
-                        for (int u = 0; u < 4; ++u) acc[i][j][4 * q + u] = __builtin_fmaf(f, __uint_as_float((uint32_t)y[u] << 16), acc[i][j][4 * q + u]);
-                    }
-            };
-            if (col < 32) add(0); else add(1);
+                            for (int u = 0; u < 4; ++u) acc[i][j][4 * q + u] = __builtin_fmaf(f, __uint_as_float((uint32_t)y[u] << 16), acc[i][j][4 * q + u]);
+                        }
+                };
+                if (col < 32) add(0); else add(1);
+            }
         }
         by_rows<FM, FN>(lds, acc, [&](int r, int c, f32x4 y) {
             const int64_t v = a.first + n + r, d = m + c;
