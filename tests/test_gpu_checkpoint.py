@@ -172,6 +172,29 @@ def test_weight_gradients(R, D, ends, pad, dtY, dtG):
     assert (wide[:, :5] == 7).all() and (wide[:, 5 + R * D:] == 7).all()
 
 
+@pytest.mark.parametrize("dtY,dtG", [(torch.bfloat16, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.float32, torch.float32)])
+@pytest.mark.parametrize("R,D,ends", [(100, 1333, [0, 9000, 9001, 15100]), (6, 1344, [0, 40, 15000]), (70, 1344, [5, 8000, 15000]), (7, 1333, [0, 7000, 15100]),
+                                      (4100, 2040, [0, 140])])
+def test_rows_worth_packing(R, D, ends, dtY, dtG):
+    """Rows that are no whole chunks, of tensors large enough (or products enough) to be packed first; the workspace ends where it says."""
+    _say("gradient of packed rows R=%d D=%d %s %s" % (R, D, dtY, dtG))
+    T, n = ends[-1] + 9, len(ends) - 1
+    codes, steps = Q.checkpoint8(_inputs(T, D, R + D).to(DEV))
+    g = torch.Generator().manual_seed(R * D)
+    dY = (torch.randn(T, R, generator=g) * torch.exp(torch.randn(T, 1, generator=g)) * 1e-3).to(dtY).to(DEV)
+    x, y = codes.double() * steps.double().repeat_interleave(Q.CHECKPOINT_GROUP, 1)[:, :D], dY.double()
+    ref = torch.stack([torch.mm(y[a:b].t().contiguous(), x[a:b]) for a, b in zip(ends, ends[1:])])
+    size = torch.stack([torch.mm(y[a:b].t().abs().contiguous(), x[a:b].abs()) for a, b in zip(ends, ends[1:])])
+    for t in (dY, steps):
+        t[:ends[0]] = float("nan")
+        t[ends[-1]:] = float("nan")
+    need = Q.checkpoint8_grad_workspace(T, n, R, D)
+    ws = torch.full((need + 256,), 0xFF, dtype=torch.uint8, device=DEV)
+    G = Q.checkpoint8_grad(dY, codes, steps, torch.tensor(ends, device=DEV), dtype=dtG, ws=ws[:need])
+    assert (ws[need:] == 0xFF).all()
+    assert ((G.cpu().double() - ref.cpu()).abs() <= _bound(ends, size.cpu(), ref.cpu(), dtG)).all()
+
+
 @pytest.mark.parametrize("n", [2, 63, 64, 65, 128, 255, 256, 257, 600])
 @pytest.mark.parametrize("how", ["ragged", "alike", "one long"])
 @pytest.mark.parametrize("dtY", [torch.bfloat16, torch.float32])

@@ -180,6 +180,21 @@ def test_certain_and_hopeless_tokens_for_dH(T, scale):
     _check(H, W, y, w, Q.token_loss(H, W, y, w))
 
 
+@pytest.mark.parametrize("T,D,V", [(1, 64, 100), (2, 2048, 32000), (4, 4096, 1000), (20, 100, 150000), (40, 200, 5000), (100, 8192, 4000), (300, 264, 3001),
+                                   (700, 100, 150000), (2000, 72, 70000), (9000, 40, 100000)])
+@pytest.mark.parametrize("want", [(False, False), (True, False), (False, True), (True, True)])
+def test_the_workspace_ends_where_it_says(T, D, V, want):
+    _say("loss workspace T=%d D=%d V=%d dH=%s dW=%s" % (T, D, V, *want))
+    H, W, y, w = _inputs(T, D, V, 14, masked=0.0)
+    W, _ = _inside(W, 1, 0) if T % 3 == 0 else (W, None)              # packed, or read in place
+    need = Q.token_loss_workspace(T, D, V, *want)
+    ws = torch.full((need + 4096,), 0xFF, dtype=torch.uint8, device=DEV)
+    got = Q.token_loss(H, W, y, w, want_dH=want[0], want_dW=want[1], ws=ws[:need])
+    assert (ws[need:] == 0xFF).all()
+    for x in got:
+        assert x is None or x.isfinite().all()
+
+
 @pytest.mark.parametrize("T", [3, 100])
 def test_no_target_at_all(T):
     _say("loss without targets T=%d" % T)
