@@ -308,3 +308,49 @@ def test_other_stream_and_shared_workspace():
         s.synchronize()
         for a, b in zip(want, got):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("T,want_dW", [(2, False), (20, True), (70, False), (1100, False), (1100, True)])
+def test_other_kernels_replayed(T, want_dW):
+    _say("loss replayed T=%d dW=%s" % (T, want_dW))
+    Q.init()
+    held = _inputs(T, 200, 1500, 9)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        Q.token_loss(*held, want_dW=want_dW)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = Q.token_loss(*held, want_dW=want_dW)
+    for i in range(3):
+        for a, b in zip(held, _inputs(T, 200, 1500, 10 + i, masked=0.25 * i)):
+            a.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        kept = [None if x is None else x.clone() for x in out]
+        for p, q in zip(kept, Q.token_loss(*held, want_dW=want_dW)):
+            assert (p is None and q is None) or torch.equal(p, q)
+
+
+def test_calls_on_two_streams_at_once():
+    """Each with a workspace of its own; results as of calls one after another."""
+    _say("loss and checkpoints on two streams")
+    sets = [_inputs(T, 264, 5000, T) for T in (700, 40)]
+    ends = [torch.tensor([0, 13, len(x[0])], device=DEV) for x in sets]
+
+    def call(x, e):
+        got = Q.token_loss(*x, want_dW=True)
+        return got + (Q.checkpoint8_grad(got[2], *Q.checkpoint8(x[0]), e),)
+    want = [call(x, e) for x, e in zip(sets, ends)]
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(3):
+        for x, e, s in zip(sets, ends, streams):
+            with torch.cuda.stream(s):
+                got.append(call(x, e))
+    torch.cuda.synchronize()
+    for i, g in enumerate(got):
+        for a, b in zip(want[i % 2], g):
+            assert torch.equal(a, b)
