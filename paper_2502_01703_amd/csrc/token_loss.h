@@ -14,9 +14,9 @@ __device__ inline void join_pair(float &top, float &sum, float top2, float sum2)
     top = next;
 }
 
-// token_loss_single.hip: the loss and dH of at most four tokens, in one pass over W, whose rows are whole 16-byte chunks.
-bool single_serves(int64_t T, int32_t D, int32_t V);
-size_t single_workspace(int64_t T, int32_t D, int32_t V);
+// token_loss_single.hip: the loss (and dH) of at most four tokens, in one pass over W, whose rows are whole 16-byte chunks.
+bool single_serves(int64_t T, int32_t D, int32_t V, bool want_dH);
+size_t single_workspace(int64_t T, int32_t D, int32_t V, bool want_dH);
 qless_status launch_single(const uint16_t *H, int64_t ldH, const uint16_t *W, int64_t ldW, int T, int32_t D, int32_t V, const int64_t *target,
                            const float *weight, float *nll, float *lse, uint16_t *dH, int64_t ldDH, void *ws, hipStream_t st);
 

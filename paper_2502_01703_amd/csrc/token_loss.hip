@@ -843,7 +843,7 @@ static qless_status logits_product(const LossPlan &p, ProductArgs a, int64_t ent
 extern "C" size_t qless_token_loss_workspace(int64_t T, int32_t D, int32_t V, int want_dH, int want_dW) {
     using namespace qless;
     if (T < 0 || D < 1 || V < 1 || D > 65536 || T > 0x3FFFFFFF || V > 0x1FFFFFFF) return 0;
-    const size_t total = loss_plan(T, D, V, want_dH != 0, want_dW != 0).total, single = want_dH ? single_workspace(T, D, V) : 0;
+    const size_t total = loss_plan(T, D, V, want_dH != 0, want_dW != 0).total, single = single_workspace(T, D, V, want_dH != 0);
     return total > single ? total : single;
 }
 
@@ -861,7 +861,7 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
     const hipStream_t st = (hipStream_t)stream;
     // W is read where it lies if its rows are whole 16-byte chunks; else a piece at a time is packed into the workspace
     const bool packs = ((uintptr_t)W & 15) != 0 || (ldW % 8 != 0 && V > 1) || D % 8 != 0 || ldW * 2 >= ((int64_t)1 << 23);
-    if (dH && !dW && !packs && single_serves(T, D, V))
+    if (!dW && !packs && single_serves(T, D, V, dH != nullptr))
         return launch_single((const uint16_t *)H, ldH, (const uint16_t *)W, V > 1 ? ldW : D, (int)T, D, V, target, weight, nll, lse, (uint16_t *)dH, ldDH, ws, st);
     const LossPlan p = loss_plan(T, D, V, dH != nullptr, dW != nullptr);
     unsigned char *base = (unsigned char *)ws;

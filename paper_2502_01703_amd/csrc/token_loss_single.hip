@@ -1,4 +1,4 @@
-// qless_token_loss of one to four tokens with dH: one pass over W.
+// qless_token_loss of one to four tokens, alone or with dH: one pass over W.
 //
 // Bound: memory, W is read once (the tile kernels read it for the logits and again for dH).  A workgroup takes a contiguous share of the
 // vocabulary, a thread 8 KU columns of all its rows, so that a row that has been multiplied with the tokens for its logits is
@@ -40,7 +40,7 @@ __device__ inline float wave_sum_last(float x) {
     return dpp_add<0x143, 0xC>(x);
 }
 
-template <int TT, int KU, int NW>
+template <int TT, int KU, int NW, bool DH>
 __global__ void __launch_bounds__(64 * NW, 2)
 loss_single_kernel(SingleArgs a) {
     constexpr int RB = (TT == 4 || TT * KU == 8 ? 4 : 8) / KU, N = RB * TT;        // as registers allow
@@ -122,6 +122,7 @@ loss_single_kernel(SingleArgs a) {
                     if (tid == 0) a.hit[t] = z[r * TT + t];
                 }
             }
+            if (!DH) continue;
 #pragma unroll
             for (int k = 0; k < KU; ++k)
 #pragma unroll
@@ -151,6 +152,7 @@ loss_single_kernel(SingleArgs a) {
     for (int t = 0; t < TT; ++t) {
         if (t >= a.T) break;
         if (tid == 0) a.part[(int64_t)blockIdx.x * a.T + t] = make_float2(top[t], sum[t]);
+        if (!DH) continue;
         float *out = a.planes + ((int64_t)blockIdx.x * a.T + t) * a.Dp;
 #pragma unroll
         for (int k = 0; k < KU; ++k)
@@ -161,7 +163,7 @@ loss_single_kernel(SingleArgs a) {
     }
 }
 
-// Grid (tokens, 16 columns): the workgroups' parts of a token joined, four columns a thread, 64 threads sharing the planes, the first of which are
+// Grid (tokens, 16 columns, or one workgroup where dH is null): the workgroups' parts of a token joined, four columns a thread, 64 threads sharing the planes, the first of which are
 // requested before the parts are (1 x 2048 x 32000: 5.6 us; with 16 threads, and none ahead, 8.3).
 __global__ void __launch_bounds__(256)
 loss_single_join_kernel(SingleArgs a, int groups) {
@@ -174,7 +176,7 @@ loss_single_join_kernel(SingleArgs a, int groups) {
     const int c = (int)blockIdx.y * 16 + (tid & 3) * 4;
     uint16_t *out = a.dH + t * a.ldDH + c;
     if (!live) {
-        if (tid < 4)
+        if (tid < 4 && a.dH)
 #pragma unroll
             for (int u = 0; u < 4; ++u) if (c + u < a.D) out[u] = 0;
         if (tid == 0 && blockIdx.y == 0) {
@@ -183,7 +185,7 @@ loss_single_join_kernel(SingleArgs a, int groups) {
         }
         return;
     }
-    const bool on = c < a.D;                               // D is a multiple of eight
+    const bool on = a.dH && c < a.D;                               // D is a multiple of eight
     auto plane = [&](int g) { return on && g < groups ? *(const float4 *)(a.planes + ((int64_t)g * a.T + t) * a.Dp + c) : make_float4(0.0f, 0.0f, 0.0f, 0.0f); };
     float4 ahead[AHEAD];
 #pragma unroll
@@ -252,10 +254,11 @@ static int single_groups(int32_t D) {          // two wavefronts a SIMD
 }
 
 // Registers: tokens and sums of 16 KU T floats next to 64 of the rows.  Three and four tokens gain where a thread's columns are sixteen, the
-// vector work then hides behind memory (4 x 4096 x 131072 415 -> 309 us, 4 x 1024 x 50257 54 -> 77), and where launches count.
-bool single_serves(int64_t T, int32_t D, int32_t V) {
+// vector work then hides behind memory (4 x 4096 x 131072 415 -> 309 us, 4 x 1024 x 50257 54 -> 77), and where launches count.  The loss alone
+// is one read of W for the tile kernels too: one token 1 x 4096 x 32000 58 -> 46 us, with cold caches 123 -> 99; two tokens 2 x 2496 x 25064 30 -> 35, 66 -> 63.
+bool single_serves(int64_t T, int32_t D, int32_t V, bool want_dH) {
     if (T < 1 || T > 4 || D > 8192 || T * single_units(D) > 8) return false;
-    return T <= 2 || (D > 2048 && D <= 4096) || (int64_t)V * D <= (4 << 20);
+    return T == 1 || (want_dH && (T == 2 || (D > 2048 && D <= 4096))) || (int64_t)V * D <= (4 << 20);
 }
 static int single_share(int32_t D, int32_t V) {            // rows of W of a workgroup: a batch at least
     const int groups = single_groups(D), share = (V + groups - 1) / groups, batch = 8 / single_units(D);
@@ -263,14 +266,16 @@ static int single_share(int32_t D, int32_t V) {            // rows of W of a wor
 }
 static int single_used(int32_t D, int32_t V) { return (V + single_share(D, V) - 1) / single_share(D, V); }       // workgroups that have rows
 static size_t single_parts(int64_t T, int32_t D, int32_t V) { return ((size_t)single_used(D, V) * T * 8 + 255) & ~(size_t)255; }
-size_t single_workspace(int64_t T, int32_t D, int32_t V) {
-    return single_serves(T, D, V) ? 256 + single_parts(T, D, V) + (size_t)single_used(D, V) * T * single_dp(D) * 4 : 0;
+size_t single_workspace(int64_t T, int32_t D, int32_t V, bool want_dH) {
+    if (!single_serves(T, D, V, want_dH)) return 0;
+    return 256 + single_parts(T, D, V) + (want_dH ? (size_t)single_used(D, V) * T * single_dp(D) * 4 : 0);
 }
 
 template <int TT, int KU, int NW>
 static void launch_single_as(const SingleArgs &a, int groups, hipStream_t st) {
-    hipLaunchKernelGGL((loss_single_kernel<TT, KU, NW>), dim3((unsigned)groups), dim3(64 * NW), 0, st, a);
-    hipLaunchKernelGGL(loss_single_join_kernel, dim3((unsigned)a.T, (unsigned)((a.D + 15) / 16)), dim3(256), 0, st, a, groups);
+    if (a.dH) hipLaunchKernelGGL((loss_single_kernel<TT, KU, NW, true>), dim3((unsigned)groups), dim3(64 * NW), 0, st, a);
+    else hipLaunchKernelGGL((loss_single_kernel<TT, KU, NW, false>), dim3((unsigned)groups), dim3(64 * NW), 0, st, a);
+    hipLaunchKernelGGL(loss_single_join_kernel, dim3((unsigned)a.T, a.dH ? (unsigned)((a.D + 15) / 16) : 1), dim3(256), 0, st, a, groups);
 }
 
 qless_status launch_single(const uint16_t *H, int64_t ldH, const uint16_t *W, int64_t ldW, int T, int32_t D, int32_t V, const int64_t *target,

@@ -354,3 +354,13 @@ def test_calls_on_two_streams_at_once():
     for i, g in enumerate(got):
         for a, b in zip(want[i % 2], g):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("T,D,V", [(1, 8, 1), (1, 64, 7), (1, 2048, 5000), (1, 4104, 1500), (1, 8192, 4097), (1, 8200, 600), (1, 16, 200000), (2, 200, 4000), (2, 4096, 1001), (3, 1000, 3000),
+                                   (4, 2048, 2049), (4, 4096, 1000), (4, 16, 100000)])
+def test_loss_alone_of_few_tokens(T, D, V):
+    _say("loss alone T=%d D=%d V=%d" % (T, D, V))
+    H, W, y, w = _inputs(T, D, V, T + D + V, masked=0.0)
+    for z in (y, torch.zeros_like(y), torch.full_like(y, V - 1), torch.full_like(y, -100)):
+        ws = torch.full((Q.token_loss_workspace(T, D, V, False),), 0xFF, dtype=torch.uint8, device=DEV)
+        _check(H, W, z, w, Q.token_loss(H, W, z, w, want_dH=False, ws=ws))
