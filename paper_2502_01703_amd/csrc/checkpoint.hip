@@ -704,18 +704,17 @@ checkpoint_join_kernel(GradArgs a) {
     }
 }
 
-// ---- Many rows of R (a layer's own weights): the products are the bound, so that the activations are formed once, as bfloat16 rows of
-// tokens, and the tiles of product.h multiply them with the gradients.  fp32 results take the activations as the sum of two bfloat16
-// numbers (exact: a code times its step has 15 bits), bfloat16 ones rounded once, which is half the products.
-// Workgroups take 64 tokens of an example (the last ones of it with zeros behind them): block e + offset[e] / 64 and on, TERMS times 64 rows each.
-template <int TERMS>
+// ---- Many rows of R (a layer's own weights) with bfloat16 results: the products are the bound, so that the activations are formed once, as
+// bfloat16 rows of tokens, rounded once, and the tiles of product.h multiply them with the gradients.  (With fp32 results both terms of an activation would
+// enter: 1 x 8192 tokens, R = D = 4096 450 us, the ring 418.)
+// Workgroups take 64 tokens of an example (the last ones of it with zeros behind them): block e + offset[e] / 64 and on.
 __global__ void __launch_bounds__(256)
 checkpoint_expand_kernel(GradArgs a, uint16_t *out, int64_t ld) {
     int64_t o0, o1;
     const int64_t j = blockIdx.x, e = find_example(a, j, 64, o0, o1);
     if (e < 0) return;
     const int64_t t0 = o0 + 64 * (j - (e + o0 / 64));
-    out += j * TERMS * 64 * ld;
+    out += j * 64 * ld;
     for (int64_t i = (int64_t)blockIdx.y * 256 + threadIdx.x; i < 64 * (ld / 8); i += (int64_t)gridDim.y * 256) {
         const int64_t r = i / (ld / 8), c = (i - r * (ld / 8)) * 8, t = t0 + r, left = t < o1 ? a.D - c : 0;
         const int8_t *in = a.codes + t * a.ldC + c;
@@ -728,25 +727,20 @@ checkpoint_expand_kernel(GradArgs a, uint16_t *out, int64_t ld) {
         float x[8];
 #pragma unroll
         for (int u = 0; u < 8; ++u) x[u] = __fmul_rn((float)q[u], s);
-#pragma unroll
-        for (int term = 0; term < TERMS; ++term) {
-            Eight<uint16_t>::store(out + (term * 64 + r) * ld + c, 8, x);
-#pragma unroll
-            for (int u = 0; u < 8; ++u) x[u] = __fsub_rn(x[u], bf16_value(bf16_bits(x[u])));
-        }
+        Eight<uint16_t>::store(out + r * ld + c, 8, x);
     }
 }
 // rows m are columns of G, columns n its rows, the part of K its example
-template <class Out> struct GradStore {
-    struct Args { Out *G; int64_t ldG; int32_t R, D; };
+struct GradStore {
+    struct Args { uint16_t *G; int64_t ldG; int32_t R, D; };
     template <int FM, int FN>
     static __device__ inline void run(const Args &a, unsigned char *lds, f32x16 (&acc)[FM][FN], int64_t m, int64_t n, int e, int64_t) {
         by_rows<FM, FN>(lds, acc, [&](int r, int c, f32x4 y) {
             const int64_t d = m + c;
             if (n + r >= a.R) return;
-            Out x[4], *out = a.G + e * a.ldG + (n + r) * a.D + d;
+            uint16_t x[4], *out = a.G + e * a.ldG + (n + r) * a.D + d;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) x[u] = sizeof(Out) == 2 ? (Out)bf16_bits(y[u]) : (Out)y[u];
+            for (int u = 0; u < 4; ++u) x[u] = bf16_bits(y[u]);
             if (d + 4 <= a.D) __builtin_memcpy(out, x, sizeof x);
             else
 #pragma unroll
@@ -757,21 +751,21 @@ template <class Out> struct GradStore {
 typedef ProductShape<256, 256, 2, 4, 2> GradTile;
 
 static int64_t expand_ld(int32_t D) { return ((int64_t)D + 7) / 8 * 8; }
-// Rows of R and examples that fill the chip with tiles, of tokens enough that padding them to 64 costs little.
+// Rows of R and examples that fill the chip with tiles (whole examples: with several of different lengths twice as well), of tokens enough that padding them to 64 costs
+// little.  16 x 32768 tokens, R = 2048, D = 1024 163 us, by the ring 225; 8 x 65536, R = D = 1024 487 and 252; 64 x 16384, R = 300, D = 2048 99 and 69.
 static bool many_rows(int64_t T, int64_t n, int32_t R, int32_t D) {
-    return R >= 256 && T >= 128 * n && n * ((R + 255) / 256) * ((D + 255) / 256) >= compute_units() / 2;
+    return R >= 1024 && T >= 128 * n && n * ((R + 255) / 256) * ((D + 255) / 256) >= (n == 1 ? compute_units() / 2 : compute_units());
 }
-static size_t expand_bytes(int64_t T, int64_t n, int32_t D, int terms) { return (size_t)(n + T / 64) * 64 * terms * (size_t)expand_ld(D) * 2; }
+static size_t expand_bytes(int64_t T, int64_t n, int32_t D) { return (size_t)(n + T / 64) * 64 * (size_t)expand_ld(D) * 2; }
 
-template <int TERMS, class Out>
 static qless_status launch_many(const GradArgs &a, hipStream_t st) {
     uint16_t *x = (uint16_t *)a.planes;
     const int64_t ld = expand_ld(a.D), blocks = a.n + a.T / 64;
-    if (blocks > 0x7FFFFFFF / (64 * TERMS)) return QLESS_ERR_UNSUPPORTED;
-    const ProductArgs p{ProductOperand{x, ld * 2, ld * 2, blocks * 64 * TERMS}, ProductOperand{a.dY, a.ldY * 2, (int64_t)a.Rc * 2, 0},
+    if (blocks > 0x7FFFFFFF / 64) return QLESS_ERR_UNSUPPORTED;
+    const ProductArgs p{ProductOperand{x, ld * 2, ld * 2, blocks * 64}, ProductOperand{a.dY, a.ldY * 2, (int64_t)a.Rc * 2, 0},
                         a.R, a.T, nullptr, nullptr, (a.D + 255) / 256, (int32_t)a.n, a.offsets, nullptr, 0, 0};
-    hipLaunchKernelGGL(checkpoint_expand_kernel<TERMS>, dim3((unsigned)blocks, (unsigned)((ld + 127) / 128)), dim3(256), 0, st, a, x, ld);
-    const qless_status rc = launch_product<GradTile, ACROSS, ACROSS, GradStore<Out>, TERMS>(p, typename GradStore<Out>::Args{(Out *)a.G, a.ldG, a.R, a.D}, st);
+    hipLaunchKernelGGL(checkpoint_expand_kernel, dim3((unsigned)blocks, (unsigned)((ld + 127) / 128)), dim3(256), 0, st, a, x, ld);
+    const qless_status rc = launch_product<GradTile, ACROSS, ACROSS, GradStore, true>(p, GradStore::Args{(uint16_t *)a.G, a.ldG, a.R, a.D}, st);
     return rc == QLESS_OK ? launch_status() : rc;
 }
 
@@ -904,7 +898,7 @@ extern "C" size_t qless_checkpoint8_grad_workspace(int64_t T, int64_t n, int32_t
     using namespace qless;
     if (T < 0 || n < 1 || R < 1 || D < 1) return 0;
     const int64_t segments = grad_segments(T, n, grad_chunk(T, n, R, D));
-    const size_t planes = segments > n ? (size_t)segments * (size_t)R * (size_t)D * 4 : 0, rows = many_rows(T, n, R, D) ? expand_bytes(T, n, D, 2) : 0;
+    const size_t planes = segments > n ? (size_t)segments * (size_t)R * (size_t)D * 4 : 0, rows = many_rows(T, n, R, D) ? expand_bytes(T, n, D) : 0;
     return up16((planes > rows ? planes : rows)) + packed_bytes(T, n, R, D);
 }
 
@@ -928,7 +922,7 @@ extern "C" qless_status qless_checkpoint8_grad(const void *dY, qless_dtype dtY, 
     const int bytes = dtY == QLESS_BF16 ? 2 : 4, rc = packed_R(R, bytes);
     if (T > 0 && T <= 0x3FFFFFFF && (int64_t)T * (rc * (int64_t)bytes / 16) < ((int64_t)1 << 38) && (int64_t)T * (packed_D(D) / 16) < ((int64_t)1 << 38)) {
         unsigned char *pack = (unsigned char *)ws + (need - packed_bytes(T, n, R, D));
-        const bool many = dtY == QLESS_BF16 && expand_ld(D) < (1 << 22) && many_rows(T, n, R, D);
+        const bool many = dtY == QLESS_BF16 && dtG == QLESS_BF16 && expand_ld(D) < (1 << 22) && many_rows(T, n, R, D);
         if (rc != R && worth_packing(T, n, R, D)) {
             if (bytes == 2) launch_pack((const uint16_t *)dY, ldY, T, R, (uint16_t *)pack, rc, st);
             else launch_pack((const float *)dY, ldY, T, R, (float *)pack, rc, st);
@@ -942,7 +936,7 @@ extern "C" qless_status qless_checkpoint8_grad(const void *dY, qless_dtype dtY, 
         }
         // 16-byte copies and 32-bit offsets
         const bool whole_y = a.Rc == rc && (T == 1 || a.ldY * bytes % 16 == 0) && ((uintptr_t)a.dY & 15) == 0 && a.ldY < (1 << 22);
-        if (whole_y && many) return dtG == QLESS_BF16 ? launch_many<1, uint16_t>(a, st) : launch_many<2, float>(a, st);
+        if (whole_y && many) return launch_many(a, st);
         if (whole_y && a.Dc % 16 == 0 && (T == 1 || a.ldC % 16 == 0) && ((uintptr_t)a.codes & 15) == 0 && a.ldC < (1 << 24) && ldS < (1 << 24)) {
             if (dtY == QLESS_BF16) return dtG == QLESS_BF16 ? launch_ring_rows<uint16_t, uint16_t>(a, st) : launch_ring_rows<uint16_t, float>(a, st);
             return dtG == QLESS_BF16 ? launch_ring_rows<float, uint16_t>(a, st) : launch_ring_rows<float, float>(a, st);

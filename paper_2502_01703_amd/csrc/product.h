@@ -32,7 +32,7 @@ struct ProductArgs {
     const int32_t *live_n, *live_k;   // device: fewer of them, or null (k rounded up to a stage: the operands are zero there)
     int32_t mtiles, splits;    // splits: K in as many parts of whole stages
     // CUTS: part e of K is the rows [cuts[e], cuts[e + 1]) of b (device; clamped to 0 .. k), its stages in a begin at stage
-    // TERMS (e + cuts[e] / 64): each 64 rows of b meet TERMS stages of a, one after another, which are zeros behind the part's rows.
+    // e + cuts[e] / 64, and are zeros behind the part's rows.
     const int64_t *cuts;
     // SHIFT: b holds numbers that are not negative, and b(n, k) is to be multiplied by a power of two for each n and each 64 << shift_stages
     // steps of K: shift[k / (64 << shift_stages)][n] takes it off the exponents of two such numbers at once (bits 7 on of each half), down
@@ -162,21 +162,45 @@ __device__ inline void by_rows(unsigned char *lds, f32x16 (&acc)[FM][FN], Store 
 
 // Epilogue::run(args, lds, acc, m, n, split, live): acc[i][j][v] is C at m + 32 i + 8 (v / 4) + 4 half + v % 4, n + 32 j + lane % 32; lds: the
 // workgroup's, free.
-template <class Sh, int AK, int BK, class Epilogue, int CUTS = 0, bool SHIFT = false>
+template <class Sh, int AK, int BK, class Epilogue, bool CUTS = false, bool SHIFT = false>
 __global__ void __launch_bounds__(64 * Sh::NW, Sh::NW / 4)
 product_kernel(ProductArgs p, typename Epilogue::Args e) {
-    constexpr int TERMS = CUTS ? CUTS : 1;
     constexpr int FM = Sh::FM, FN = Sh::FN, NS = Sh::NS, NW = Sh::NW;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     // Tiles in an order in which the workgroups of an XCD (ids eight apart) share operands: bands of eight column tiles, row tile by row
     // tile, an eighth of the order each.
     const int64_t n = p.live_n ? *p.live_n : p.n;
     const int64_t k = p.live_k ? *p.live_k : p.k;
-    const int64_t ntiles = (n + Sh::NT - 1) / Sh::NT, plane = p.mtiles * ntiles, total = plane * p.splits, per = (total + 7) / 8;
-    const int64_t id = blockIdx.x, idx = (id & 7) * per + (id >> 3);
-    if ((id >> 3) >= per || idx >= total) return;          // the whole workgroup
-    const int split = __builtin_amdgcn_readfirstlane((int)(idx / plane));
-    const int64_t in = idx - split * plane, band = in / (8 * p.mtiles), wide = ntiles - band * 8 < 8 ? ntiles - band * 8 : 8, r = in - band * 8 * p.mtiles;
+    // CUTS: an eighth of every part, whose lengths differ, or a whole one of at most eight tiles, from the longest to the shortest (up to 64).
+    const int64_t ntiles = (n + Sh::NT - 1) / Sh::NT, plane = p.mtiles * ntiles, total = plane * p.splits;
+    const int64_t xcd = blockIdx.x & 7, q = blockIdx.x >> 3;
+    int64_t in;
+    int split;
+    if (CUTS) {
+        const int64_t per = plane <= 8 ? plane : (plane + 7) / 8, at = q / per, part = plane <= 8 ? at * 8 + xcd : at;
+        // (an eighth of fewer tiles begins where the part before ended)
+        in = plane <= 8 ? q - at * per : ((xcd + at * (8 - (plane + per - 1) / per)) & 7) * per + q - at * per;
+        if (part >= p.splits || in >= plane) return;       // the whole workgroup
+        split = __builtin_amdgcn_readfirstlane((int)part);
+    } else {
+        const int64_t per = (total + 7) / 8, idx = xcd * per + q;
+        if (q >= per || idx >= total) return;
+        split = __builtin_amdgcn_readfirstlane((int)(idx / plane));
+        in = idx - split * plane;
+    }
+    if (CUTS && p.splits > 1 && p.splits <= 64) {
+        const int lane = threadIdx.x & 63;
+        const int64_t len = lane < p.splits ? p.cuts[lane + 1] - p.cuts[lane] : -1;
+        const int key = len < 0 ? -1 : len < 0x7FFFFFFF ? (int)len : 0x7FFFFFFF;
+        int longer = 0;
+        for (int i = 0; i < p.splits; ++i) {
+            const int other = __builtin_amdgcn_readlane(key, i);
+            longer += other > key || (other == key && i < lane);
+        }
+        split = __ffsll((unsigned long long)__ballot(lane < p.splits && longer == split)) - 1;      // (a total order: one lane)
+        split = __builtin_amdgcn_readfirstlane(split);
+    }
+    const int64_t band = in / (8 * p.mtiles), wide = ntiles - band * 8 < 8 ? ntiles - band * 8 : 8, r = in - band * 8 * p.mtiles;
     const int m0 = __builtin_amdgcn_readfirstlane((int)(r / wide * Sh::MT)), n0 = __builtin_amdgcn_readfirstlane((int)((band * 8 + r % wide) * Sh::NT));
     const int64_t stages = (k + 63) / 64;
     int s0 = __builtin_amdgcn_readfirstlane((int)(stages * split / p.splits)), s1 = __builtin_amdgcn_readfirstlane((int)(stages * (split + 1) / p.splits));
@@ -186,8 +210,8 @@ product_kernel(ProductArgs p, typename Epilogue::Args e) {
         lo = lo < 0 ? 0 : (lo > k ? k : lo);
         hi = hi < lo ? lo : (hi > k ? k : hi);
         const int64_t block = split + lo / 64;
-        s0 = __builtin_amdgcn_readfirstlane((int)block * TERMS);
-        s1 = s0 + __builtin_amdgcn_readfirstlane((int)((hi - lo + 63) / 64) * TERMS);
+        s0 = __builtin_amdgcn_readfirstlane((int)block);
+        s1 = s0 + __builtin_amdgcn_readfirstlane((int)((hi - lo + 63) / 64));
         p.b.base = (const unsigned char *)p.b.base + (lo - 64 * block) * p.b.ld;      // stage s0 begins at row lo
         p.b.depth = 64 * block + hi - lo;
     }
@@ -205,7 +229,7 @@ product_kernel(ProductArgs p, typename Epilogue::Args e) {
         if (s > s1 - 1) s = s1 - 1;
         const unsigned at = lds0 + (unsigned)(slot * Sh::STAGE);
         if (u < UA) ca.issue(u, s, lane, wave, at);
-        else if (u < UA + UB) cb.issue(u - UA, s / TERMS, lane, wave, at + Sh::MT * 128);
+        else if (u < UA + UB) cb.issue(u - UA, s, lane, wave, at + Sh::MT * 128);
         else                                               // this wavefront's columns' shifts
             global_to_lds4(p.shift + (int64_t)(s >> p.shift_stages) * p.shift_ld + n0 + nb, (unsigned)((lane & (32 * FN - 1)) * 4), lds0 + (unsigned)(NS * Sh::STAGE + (slot * NW + wave) * 256));
     };
@@ -289,12 +313,13 @@ product_kernel(ProductArgs p, typename Epilogue::Args e) {
     Epilogue::template run<FM, FN>(e, smem, acc, m0 + ma, n0 + nb, split, n);
 }
 
-template <class Sh, int AK, int BK, class Epilogue, int CUTS = 0, bool SHIFT = false>
+template <class Sh, int AK, int BK, class Epilogue, bool CUTS = false, bool SHIFT = false>
 static qless_status launch_product(const ProductArgs &p, const typename Epilogue::Args &e, hipStream_t st) {
     constexpr int LDS = Sh::LDS + (SHIFT ? Sh::NS * Sh::NW * 256 : 0);
     static_assert(LDS <= 160 * 1024, "the stages fit");
     QLESS_LDS_KERNEL((product_kernel<Sh, AK, BK, Epilogue, CUTS, SHIFT>), LDS);
-    const int64_t total = p.mtiles * ((p.n + Sh::NT - 1) / Sh::NT) * p.splits, grid = (total + 7) / 8 * 8;
+    const int64_t total = p.mtiles * ((p.n + Sh::NT - 1) / Sh::NT) * p.splits, plane = total / p.splits;
+    const int64_t grid = !CUTS ? (total + 7) / 8 * 8 : plane <= 8 ? (p.splits + 7) / 8 * 8 * plane : (plane + 7) / 8 * 8 * p.splits;
     if (grid > 0x7FFFFFFF) return QLESS_ERR_UNSUPPORTED;
     if (grid > 0)
         hipLaunchKernelGGL((product_kernel<Sh, AK, BK, Epilogue, CUTS, SHIFT>), dim3((unsigned)grid), dim3(64 * Sh::NW), LDS, st, p, e);

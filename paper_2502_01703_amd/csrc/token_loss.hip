@@ -825,9 +825,9 @@ static qless_status loss_product(int tile_n, const ProductArgs &a, const typenam
         case 32:
             if constexpr (FROM == 32) return launch_product<Loss32, AK, BK, Epilogue>(a, e, st);
             return QLESS_ERR_UNSUPPORTED;
-        case 64: return launch_product<std::conditional_t<SHIFT, LossShift, Loss64>, AK, BK, Epilogue, 0, SHIFT>(a, e, st);
-        case 128: return launch_product<Loss128, AK, BK, Epilogue, 0, SHIFT>(a, e, st);
-        default: return launch_product<Loss256, AK, BK, Epilogue, 0, SHIFT>(a, e, st);
+        case 64: return launch_product<std::conditional_t<SHIFT, LossShift, Loss64>, AK, BK, Epilogue, false, SHIFT>(a, e, st);
+        case 128: return launch_product<Loss128, AK, BK, Epilogue, false, SHIFT>(a, e, st);
+        default: return launch_product<Loss256, AK, BK, Epilogue, false, SHIFT>(a, e, st);
     }
 }
 // the tiles of logits of `entries` from the vocabulary

@@ -195,6 +195,26 @@ def test_rows_worth_packing(R, D, ends, dtY, dtG):
     assert ((G.cpu().double() - ref.cpu()).abs() <= _bound(ends, size.cpu(), ref.cpu(), dtG)).all()
 
 
+@pytest.mark.parametrize("n,R,D", [(4, 2048, 2048), (5, 2045, 1800), (32, 1024, 512), (22, 1536, 512), (65, 1024, 250), (33, 1100, 264), (9, 4096, 500)])
+@pytest.mark.parametrize("how", ["ragged", "alike"])
+def test_many_rows_of_many_examples(n, R, D, how):
+    """Expanded activations and tiles of whole examples, ranked by length up to 64 of them; empty ones, and ones that end in a stage."""
+    _say("gradient of many rows n=%d R=%d D=%d %s" % (n, R, D, how))
+    g = torch.Generator().manual_seed(n)
+    T = 130 * n
+    ends = [130 * e for e in range(n + 1)]
+    if how == "ragged":
+        ends = [3] + torch.sort(torch.randint(3, T, (n - 3,), generator=g)).values.tolist() + [T, T, T + 1]
+        T += 1
+    codes, steps = Q.checkpoint8(_inputs(T, D, R + D).to(DEV))
+    dY = (torch.randn(T, R, generator=g) * torch.exp(torch.randn(T, 1, generator=g)) * 1e-3).bfloat16().to(DEV)
+    x, y = codes.double() * steps.double().repeat_interleave(Q.CHECKPOINT_GROUP, 1)[:, :D], dY.double()
+    G = Q.checkpoint8_grad(dY, codes, steps, torch.tensor(ends, device=DEV), dtype=torch.bfloat16)
+    for e, (a, b) in enumerate(zip(ends, ends[1:])):
+        ref, size = torch.mm(y[a:b].t().contiguous(), x[a:b]), torch.mm(y[a:b].t().abs().contiguous(), x[a:b].abs())
+        assert ((G[e].double() - ref).abs().cpu() <= _bound([a, b], size[None].cpu(), ref[None].cpu(), torch.bfloat16)[0]).all(), "example %d" % e
+
+
 @pytest.mark.parametrize("n", [2, 63, 64, 65, 128, 255, 256, 257, 600])
 @pytest.mark.parametrize("how", ["ragged", "alike", "one long"])
 @pytest.mark.parametrize("dtY", [torch.bfloat16, torch.float32])
