@@ -20,6 +20,7 @@
 #include "product.h"
 #include "score.h"
 #include "token_loss.h"
+#include <cmath>
 #include <type_traits>
 
 namespace qless {
@@ -793,7 +794,10 @@ static LossPlan loss_plan(int64_t T, int32_t D, int32_t V, bool want_dH, bool wa
     p.parts = (want_dH && !p.one_pass ? piece : p.Vp) / p.per_part;
     const int64_t tiles = ((D + 255) / 256) * ntiles, stages = piece / 64;
     int64_t splits = tiles > 0 ? cus / tiles : 1;
-    if (splits > stages / 8) splits = stages / 8;
+    // a stage takes 1.3 us, a plane its bytes' time twice (512 x 512 x 2000: 45 us with eight stages a split at least, 42 with four; 1024 x 1024 x 5000: 61 and 68, so by both)
+    const int64_t worth = (int64_t)sqrt((double)stages * 1.3 * 5e6 / (8.0 * (double)(T > 0 ? T : 1) * (double)p.Dp));
+    if (splits > stages / 4) splits = stages / 4;
+    if (splits > worth) splits = worth;
     if (splits < 1) splits = 1;
     p.splits = (int32_t)splits;
     size_t at = 0;
