@@ -847,8 +847,14 @@ static qless_status logits_product(const LossPlan &p, ProductArgs a, int64_t ent
 extern "C" size_t qless_token_loss_workspace(int64_t T, int32_t D, int32_t V, int want_dH, int want_dW) {
     using namespace qless;
     if (T < 0 || D < 1 || V < 1 || D > 65536 || T > 0x3FFFFFFF || V > 0x1FFFFFFF) return 0;
-    const size_t total = loss_plan(T, D, V, want_dH != 0, want_dW != 0).total, single = single_workspace(T, D, V, want_dH != 0);
-    return total > single ? total : single;
+    // (a workspace for more outputs serves fewer, which may keep the parts of a whole vocabulary where more pass a piece at a time)
+    size_t most = single_workspace(T, D, V, want_dH != 0);
+    for (int some = 0; some < 4; ++some) {
+        if (((some & 1) && !want_dH) || ((some & 2) && !want_dW)) continue;
+        const size_t total = loss_plan(T, D, V, (some & 1) != 0, (some & 2) != 0).total;
+        if (total > most) most = total;
+    }
+    return most;
 }
 
 extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void *W, int64_t ldW, qless_dtype dt, int64_t T, int32_t D, int32_t V,

@@ -1,5 +1,6 @@
 """The loss over the vocabulary, without a GPU: what the entry point refuses."""
 import ctypes
+import random
 
 from paper_2502_01703_amd import binding
 
@@ -45,3 +46,11 @@ def test_a_workspace_for_more_outputs_serves_fewer():
     for T, D, V in ((1, 64, 100), (1, 4096, 32000), (2, 8192, 7), (4, 4096, 1000), (31, 100, 5000), (40, 8192, 4000), (300, 264, 3001), (9000, 40, 100000)):
         loss, dH, dW, both = (L.qless_token_loss_workspace(T, D, V, *want) for want in ((0, 0), (1, 0), (0, 1), (1, 1)))
         assert 0 < loss <= dH <= both and loss <= dW <= both
+
+
+def test_a_workspace_for_more_outputs_serves_fewer_at_random_sizes():
+    L, r = binding.lib(), random.Random(1)
+    for _ in range(5000):
+        T, D, V = (int(2 ** r.uniform(0, top)) for top in (17, 13, 19))
+        loss, dH, dW, both = (L.qless_token_loss_workspace(T, D, V, *want) for want in ((0, 0), (1, 0), (0, 1), (1, 1)))
+        assert 0 < loss <= dH <= both and loss <= dW <= both, (T, D, V)
