@@ -917,7 +917,7 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
     };
     auto head_product = [&](int64_t n, int64_t v0) {        // dW: rows m columns of H, columns n entries
         ProductArgs a{ProductOperand{w.H, p.Dp * 2, p.Dp * 2, p.Tp}, ProductOperand{w.delta, piece * 2, up_to(n, 64) * 2, few ? 2 * kFew : p.Tp},
-                      n, T == 0 ? 0 : few ? 2 * kFew : p.Tp, nullptr, few ? nullptr : w.count, (D + 255) / 256, 1, nullptr, nullptr, 0, 0};
+                      n, p.Tp, nullptr, w.count, (D + 255) / 256, 1, nullptr, nullptr, 0, 0};             // (without live tokens delta may be unwritten: no stage)
         const LossHead::Args e{(uint16_t *)dW, ldDW, v0, V, D, w.order, w.order_target, w.start, w.pull, w.H, p.Dp};
         if (a.mtiles * ((n + 255) / 256) < compute_units()) {            // 512 x 512 x 2000: 104 -> 86 us; a chip full of the larger ones is 5 % faster
             a.mtiles = (D + 127) / 128;
