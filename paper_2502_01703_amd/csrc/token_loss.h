@@ -4,8 +4,13 @@
 
 namespace qless {
 
-// near 0 the loss keeps its digits
-__device__ inline float loss_of(float top, float sum, float hit) { return logf(sum) + (top - hit); }
+// What follows from a token's greatest logit, the sum of exp(z - top) over the entries other than its target, and the target's logit.  With
+// the target's 1 in the sum, a loss would be rounded to steps of 2^-23, and 1 - p_target with it; apart from it, both keep their digits.
+struct TokenResult { float nll, lse, scale, pull; };        // scale, pull: of the others' sum of exp(z - top) W, and of W_target, in dH
+__device__ inline TokenResult token_result(float top, float others, float hit, float weight) {
+    const float mine = __expf(hit - top), total = others + mine, scale = weight / total;
+    return TokenResult{others < mine ? log1pf(others / mine) : logf(total) + (top - hit), top + logf(total), scale, -scale * others};
+}
 // Maximum and sum (relative to it) joined with another such pair.
 __device__ inline void join_pair(float &top, float &sum, float top2, float sum2) {
     const float next = fmaxf(top, top2);

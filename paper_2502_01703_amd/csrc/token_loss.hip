@@ -14,7 +14,7 @@
 // dW needs the sums first, and its operand's factors are not of its entries but of its tokens.  Where the whole vocabulary is one piece,
 // its logits are kept until delta is formed from them; else a second pass forms them again.
 //
-// The target's entry, the largest of a row, never passes through the bfloat16 operand: it is added in fp32, to dH in the last kernel,
+// The target's entry, the largest of a row, never passes through the bfloat16 operand, and its exponential enters no sum: it is added in fp32, to dH in the last kernel,
 // to dW behind the product, from the tokens ordered by target.  (Rounded with the rest it made gradients of few tokens up to 0.4 %
 // wrong.)  Up to 32 tokens, where the products wait for W anyway, the rest goes in as the sum of two bfloat16 numbers.
 #include "product.h"
@@ -33,7 +33,7 @@ struct LossTokens {                        // workspace views, by live token (pa
     float *weight, *lse, *hit;             // [Tp]; hit: the target's logit
     float *top, *sum, *shrink;             // [Tp] R, sum of the others' 2^(z log2 e - R), 2^ the last change of R (few tokens: of exp and m)
     float *pull;                           // [Tp] w (p_target - 1)
-    float2 *part;                          // [parts][Tp] maximum, sum of exp(z - maximum); or r, sum of the others' p
+    float2 *part;                          // [parts][Tp] maximum, sum of the others' exp(z - maximum); or r, sum of the others' p
     uint32_t *shift;                       // [parts][Tp] R - r, for two exponents
     int32_t *order, *order_target, *start; // [Tp] live tokens by target, and their targets; [Vp / 64 + 1]: where each 64 entries begin there
     float *logits;                         // [Tp][piece]
@@ -200,7 +200,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 __device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // ---- what the tiles of logits end with: rows m are vocabulary entries, columns n tokens
-// STORE: the logits too, for a delta kernel
+// The maximum, the sum of the exponentials without the target's, and the target's logit.  STORE: the logits too, for a delta kernel, -infinity the target's
 template <bool STORE> struct LossStats {
     struct Args { const int32_t *target; float *hit; float2 *part; int64_t Tp, first; int32_t V; float *logits; int64_t ld; };
     template <int FM, int FN>
@@ -213,14 +213,6 @@ template <bool STORE> struct LossStats {
             const int64_t t = n + 32 * j + l32;
             const int y = t < live ? a.target[t] - v0 : -1;
             const bool here = y >= 0 && y < 32 * FM && (y & 4) == 0;
-            if (__any(here)) {
-                float hit = 0.0f;
-#pragma unroll
-                for (int i = 0; i < FM; ++i)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) hit = y == 32 * i + 8 * (v >> 2) + (v & 3) ? acc[i][j][v] : hit;
-                if (here) a.hit[t] = hit;
-            }
             if (over < 32 * FM) {                           // the end of the vocabulary
 #pragma unroll
                 for (int i = 0; i < FM; ++i)
@@ -234,6 +226,18 @@ template <bool STORE> struct LossStats {
                 for (int v = 0; v < 16; ++v) top = fmaxf(top, acc[i][j][v]);
             top = fmaxf(top, __shfl_xor(top, 32, 64));
             const float ref = (top == -INFINITY ? 0.0f : top) * kLog2e;
+            if (__any(here)) {
+                float hit = 0.0f;
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const bool it = y == 32 * i + 8 * (v >> 2) + (v & 3);
+                        hit = it ? acc[i][j][v] : hit;
+                        acc[i][j][v] = it ? -INFINITY : acc[i][j][v];
+                    }
+                if (here) a.hit[t] = hit;
+            }
             float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < FM; ++i)
@@ -431,16 +435,16 @@ loss_join_kernel(LossTokens w, int64_t Tp, int64_t parts, float *nll, float *lse
         __syncthreads();
     }
     if (part == 0 && t < live) {
-        const float all = s_top[tok] + logf(s_sum[tok]), one = loss_of(s_top[tok], s_sum[tok], w.hit[t]);
+        const TokenResult it = token_result(s_top[tok], s_sum[tok], w.hit[t], w.weight[t]);
         const int64_t at = w.token[t];
-        w.lse[t] = all;
-        w.pull[t] = w.weight[t] * expm1f(-one);
-        nll[at] = one;
-        if (lse) lse[at] = all;
+        w.lse[t] = it.lse;
+        w.pull[t] = it.pull;
+        nll[at] = it.nll;
+        if (lse) lse[at] = it.lse;
     }
 }
 
-// A token's logits of a piece become an operand of the products, without the target's entry.  Grid (tokens, shares of the row).
+// A token's logits of a piece become an operand of the products; the target's is -infinity there.  Grid (tokens, shares of the row).
 //   RUN      p = exp(z - m), m the maximum so far; top, sum, shrink go on (one share)
 //   else     delta = w exp(z - lse), with its loss (the piece is the vocabulary; the parts hold sums)
 //   FEW      in two terms, rows t and t + kFew
@@ -470,9 +474,7 @@ loss_delta_kernel(LossTokens w, int64_t Tp, int64_t parts, int64_t first, int64_
         for (int64_t c = c0 + 4 * tid; c < c1; c += 1024) put(c, zero);
         return;
     }
-    const int64_t y = w.target[t] - first;
     const float *z = w.logits + t * ld;
-    float ref, scale = 1.0f;
     if (RUN) {
         const float before = first ? w.top[t] : -INFINITY, sum_before = first ? w.sum[t] : 0.0f;
         float top = before;
@@ -482,7 +484,7 @@ loss_delta_kernel(LossTokens w, int64_t Tp, int64_t parts, int64_t first, int64_
         if ((tid & 63) == 0) s_top[tid >> 6] = top;
         __syncthreads();
         top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
-        ref = top == -INFINITY ? 0.0f : top;
+        const float ref = top == -INFINITY ? 0.0f : top;
         float sum = 0.0f;
         for (int64_t c = 4 * tid; c < width; c += 1024) {
             const float4 v = *(const float4 *)(z + c);
@@ -492,7 +494,6 @@ loss_delta_kernel(LossTokens w, int64_t Tp, int64_t parts, int64_t first, int64_
             for (int u = 0; u < 4; ++u) {
                 x[u] = __expf(f[u] - ref);
                 sum += x[u];
-                if (c + u == y) x[u] = 0.0f;
             }
             put(c, x);
         }
@@ -523,21 +524,19 @@ loss_delta_kernel(LossTokens w, int64_t Tp, int64_t parts, int64_t first, int64_
     top = s_top[0]; sum = s_sum[0];
 #pragma unroll
     for (int i = 1; i < 4; ++i) join_pair(top, sum, s_top[i], s_sum[i]);
-    ref = top + logf(sum);
-    scale = w.weight[t];
+    const TokenResult it = token_result(top, sum, w.hit[t], w.weight[t]);
     if (tid == 0 && blockIdx.y == 0) {
-        const float one = loss_of(top, sum, w.hit[t]);
         const int64_t at = w.token[t];
-        w.pull[t] = scale * expm1f(-one);
-        nll[at] = one;
-        if (lse) lse[at] = ref;
+        w.pull[t] = it.pull;
+        nll[at] = it.nll;
+        if (lse) lse[at] = it.lse;
     }
     for (int64_t c = c0 + 4 * tid; c < c1; c += 1024) {
         const float4 v = *(const float4 *)(z + c);
         const float f[4] = {v.x, v.y, v.z, v.w};
         float x[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) x[u] = c + u == y ? 0.0f : scale * __expf(f[u] - ref);
+        for (int u = 0; u < 4; ++u) x[u] = it.scale * __expf(f[u] - top);
         put(c, x);
     }
 }
@@ -550,21 +549,24 @@ loss_gather_kernel(LossTokens w, int64_t Tp, int64_t Vp, int raw, int32_t V) {
     __shared__ float s_top[4], s_sum[4];
     const int64_t t = blockIdx.x;
     if (t >= *w.count) return;
-    const int c = (int)blockIdx.y * kGather + 4 * (int)threadIdx.x;
+    const int c = (int)blockIdx.y * kGather + 4 * (int)threadIdx.x, y = w.target[t] - c;
     f32x4 z = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
     if (c < Vp) {
         z = *(const f32x4 *)(w.raw + t * Vp + c);
 #pragma unroll 4
         for (int s = 1; s < raw; ++s) z += *(const f32x4 *)(w.raw + (s * Tp + t) * Vp + c);
-        const int y = w.target[t] - c;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (u == y) w.hit[t] = z[u];
+        for (int u = 0; u < 4; ++u)
             if (c + u >= V) z[u] = -INFINITY;
-        }
-        if (WHAT == LOGITS) *(f32x4 *)(w.logits + t * Vp + c) = z;
     }
     float top = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]));
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+        if (u == y) {
+            w.hit[t] = z[u];
+            z[u] = -INFINITY;
+        }
+    if (WHAT == LOGITS && c < Vp) *(f32x4 *)(w.logits + t * Vp + c) = z;
 #pragma unroll
     for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
     if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = top;
@@ -573,10 +575,7 @@ loss_gather_kernel(LossTokens w, int64_t Tp, int64_t Vp, int raw, int32_t V) {
     float ref = top == -INFINITY ? 0.0f : top, p[4];
     if (WHAT == POWERS) ref = ceilf(ref * kLog2e);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        if (WHAT == POWERS) p[u] = w.target[t] == c + u ? 0.0f : exp2_of(__builtin_fmaf(z[u], kLog2e, -ref));
-        else p[u] = __expf(z[u] - ref);
-    }
+    for (int u = 0; u < 4; ++u) p[u] = WHAT == POWERS ? exp2_of(__builtin_fmaf(z[u], kLog2e, -ref)) : __expf(z[u] - ref);
     if (WHAT == POWERS && c < Vp) {
         uint16_t d[4];
 #pragma unroll
@@ -671,18 +670,18 @@ loss_hidden_kernel(LossTokens w, int64_t Tp, int64_t Dp, int32_t D, int splits, 
         row += w.target[r] * ldW;
         if (run) {
             float one, all;
-            if (run == 2) {                                 // powers of two, the target apart: small losses and 1 - p_target keep their digits
+            if (run == 2) {                                 // token_result with powers of two
                 const float top = w.top[r], others = w.sum[r], at = __builtin_fmaf(w.hit[r], kLog2e, -top), mine = exp2_of(at), total = others + mine;
                 one = others < mine ? log1pf(others / mine) : kLn2 * (log2f(total) - at);
                 all = one + w.hit[r];
                 scale = w.weight[r] / total;
                 pull = -scale * others;
             } else {
-                const float top = w.top[r], sum = w.sum[r];
-                one = loss_of(top, sum, w.hit[r]);
-                all = top + logf(sum);
-                scale = w.weight[r] / sum;
-                pull = w.weight[r] * expm1f(-one);
+                const TokenResult it = token_result(w.top[r], w.sum[r], w.hit[r], w.weight[r]);
+                one = it.nll;
+                all = it.lse;
+                scale = it.scale;
+                pull = it.pull;
             }
             if (threadIdx.x == 0 && blockIdx.y == 0) {
                 nll[t] = one;

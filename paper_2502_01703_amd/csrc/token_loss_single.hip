@@ -3,7 +3,7 @@
 // Bound: memory, W is read once (the tile kernels read it for the logits and again for dH).  A workgroup takes a contiguous share of the
 // vocabulary, a thread 8 KU columns of all its rows, so that a row that has been multiplied with the tokens for its logits is
 // still in registers when its probability is known: batches of RB rows (16 to 32 KB) are requested one ahead, their logits summed over the
-// workgroup, and acc = acc exp(m_before - m) + sum_v exp(z_v - m) W_v with the running maximum m, all in fp32.  The vector units take
+// workgroup, and acc = acc exp(m_before - m) + sum_v exp(z_v - m) W_v (v not the target) with the running maximum m, all in fp32.  The vector units take
 // 4 + 4 T operations for two columns of a row, a third of the memory's time for one token and about as long for four.  The workgroups' maxima,
 // sums and rows of acc are joined by a second kernel, which adds the target's part.
 #include "token_loss.h"
@@ -116,11 +116,11 @@ loss_single_kernel(SingleArgs a) {
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
                 p[r] = __expf(z[r * TT + t] - ref);
-                sum[t] += p[r];
                 if (v + r == y[t] && v + r < v1) {         // the same for the workgroup
                     p[r] = 0.0f;
                     if (tid == 0) a.hit[t] = z[r * TT + t];
                 }
+                sum[t] += p[r];
             }
             if (!DH) continue;
 #pragma unroll
@@ -233,16 +233,16 @@ loss_single_join_kernel(SingleArgs a, int groups) {
         const float4 x = s_acc[g * 4 + tid];
         s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
     }
-    const float one = loss_of(top, sum, hit), scale = w / sum, pull = w * expm1f(-one);
+    const TokenResult it = token_result(top, sum, hit, w);
     if (tid == 0 && blockIdx.y == 0) {
-        a.nll[t] = one;
-        if (a.lse) a.lse[t] = top + logf(sum);
+        a.nll[t] = it.nll;
+        if (a.lse) a.lse[t] = it.lse;
     }
     if (!on) return;
     const float f[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-        out[u] = __builtin_bit_cast(uint16_t, (__bf16)__builtin_fmaf(pull, low_half(of_target[u]), scale * f[u]));
+        out[u] = __builtin_bit_cast(uint16_t, (__bf16)__builtin_fmaf(it.pull, low_half(of_target[u]), it.scale * f[u]));
 }
 
 static int64_t single_dp(int32_t D) { return ((int64_t)D + 7) / 8 * 8; }
