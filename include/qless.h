@@ -329,7 +329,7 @@ qless_status qless_score_groups(const void *const *train_codes, const float *con
  * of H and its weight are not read as numbers.
  *   H, dH      device, T x D bfloat16, leading dimensions ldH, ldDH >= D
  *   W, dW      device, V x D bfloat16, leading dimensions ldW, ldDW >= D
- *   dt         QLESS_BF16 (others: QLESS_ERR_UNSUPPORTED);  1 <= D <= 65536,  T < 2^30,  V < 2^29
+ *   dt         QLESS_BF16 (others: QLESS_ERR_UNSUPPORTED);  1 <= D <= 65536,  T <= 2^24 - 256,  V < 2^29,  T D < 2^39 (in whole tiles of 256)
  *   target     device, T int64           weight   device, T fp32 (the inverse of an example's count of targets, say), or NULL: 1
  *   nll        device, T fp32            lse      device, T fp32, or NULL
  *   dH, dW     either or both may be NULL; both are written whole, not added to

@@ -100,6 +100,8 @@ qless_status topk_scratch_address(void **out);
 inline qless_status launch_status() {
     return hipGetLastError() == hipSuccess ? QLESS_OK : QLESS_ERR_DEVICE;
 }
+// A launch takes fewer than 2^32 threads a dimension; more are an error of the runtime, after what was launched before.
+inline bool launchable(int64_t workgroups, int threads) { return workgroups <= (int64_t)0xFFFFFFFF / threads; }
 inline bool valid_bits(int bits) { return bits == 1 || bits == 2 || bits == 4 || bits == 8; }
 
 // quantize.hip: Eq.(4),(5) over n rows whose value at (row, m) is the sum, in ascending s, of

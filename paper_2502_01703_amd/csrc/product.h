@@ -320,7 +320,7 @@ static qless_status launch_product(const ProductArgs &p, const typename Epilogue
     QLESS_LDS_KERNEL((product_kernel<Sh, AK, BK, Epilogue, CUTS, SHIFT>), LDS);
     const int64_t total = p.mtiles * ((p.n + Sh::NT - 1) / Sh::NT) * p.splits, plane = total / p.splits;
     const int64_t grid = !CUTS ? (total + 7) / 8 * 8 : plane <= 8 ? (p.splits + 7) / 8 * 8 * plane : (plane + 7) / 8 * 8 * p.splits;
-    if (grid > 0x7FFFFFFF) return QLESS_ERR_UNSUPPORTED;
+    if (!launchable(grid, 64 * Sh::NW)) return QLESS_ERR_UNSUPPORTED;
     if (grid > 0)
         hipLaunchKernelGGL((product_kernel<Sh, AK, BK, Epilogue, CUTS, SHIFT>), dim3((unsigned)grid), dim3(64 * Sh::NW), LDS, st, p, e);
     return QLESS_OK;

@@ -53,6 +53,8 @@ constexpr int kGather = 1024;              // entries of a part where partial lo
 constexpr int kFew = 32;                   // tokens up to which the rest of delta is two terms: rows t and t + kFew of delta and H
 
 constexpr int64_t kMostEntries = 1 << 22;  // of a piece: 32-bit offsets into a tile's rows of delta
+constexpr int64_t kMostTokens = (1 << 24) - 256;           // 256 threads for each of them, up to whole tiles
+constexpr int64_t kMostTiles = (1 << 23) - 8;              // of 512 threads
 constexpr int kLossThreads = 1024;
 
 // A row of D numbers, or none, and zeros up to ld (a multiple of 64), eight elements a thread.
@@ -841,11 +843,16 @@ static qless_status logits_product(const LossPlan &p, ProductArgs a, int64_t ent
     return loss_product<Epilogue, ALONG, ALONG, FROM>(p.tile_n, a, e, st);
 }
 
+// Sizes that the launches bear: a workgroup for a token, and tiles of dH for all of them at once.
+static bool loss_sizes_ok(int64_t T, int32_t D, int32_t V) {
+    return D <= 65536 && V <= 0x1FFFFFFF && T <= kMostTokens && (D + 255) / 256 * ((T + 255) / 256) <= kMostTiles;
+}
+
 }  // namespace qless
 
 extern "C" size_t qless_token_loss_workspace(int64_t T, int32_t D, int32_t V, int want_dH, int want_dW) {
     using namespace qless;
-    if (T < 0 || D < 1 || V < 1 || D > 65536 || T > 0x3FFFFFFF || V > 0x1FFFFFFF) return 0;
+    if (T < 0 || D < 1 || V < 1 || !loss_sizes_ok(T, D, V)) return 0;
     // (a workspace for more outputs serves fewer, which may keep the parts of a whole vocabulary where more pass a piece at a time)
     size_t most = single_workspace(T, D, V, want_dH != 0);
     for (int some = 0; some < 4; ++some) {
@@ -861,7 +868,7 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
                                          void *dW, int64_t ldDW, void *ws, size_t ws_bytes, void *stream) {
     using namespace qless;
     if (T < 0 || D < 1 || V < 1 || (T > 1 && (ldH < D || (dH && ldDH < D))) || (V > 1 && (ldW < D || (dW && ldDW < D)))) return QLESS_ERR_INVALID_ARG;
-    if (dt != QLESS_BF16 || D > 65536 || T > 0x3FFFFFFF || V > 0x1FFFFFFF) return QLESS_ERR_UNSUPPORTED;
+    if (dt != QLESS_BF16 || !loss_sizes_ok(T, D, V)) return QLESS_ERR_UNSUPPORTED;
     if (T == 0 && !dW) return QLESS_OK;
     if (!W || (T > 0 && (!H || !target || !nll))) return QLESS_ERR_INVALID_ARG;
     if (!ws || ws_bytes < qless_token_loss_workspace(T, D, V, dH != nullptr, dW != nullptr) || ((uintptr_t)ws & 15) != 0) return QLESS_ERR_WORKSPACE;
@@ -885,7 +892,11 @@ extern "C" qless_status qless_token_loss(const void *H, int64_t ldH, const void 
 
     const bool gradient = dH || dW, few = T <= kFew;
     const int64_t bytes = p.one_pass ? 6 : 2;
-    int64_t piece = gradient ? p.piece : p.Vp;
+    int64_t piece = p.piece;
+    if (!gradient) {                                        // the vocabulary at once, but for more tiles than a launch takes
+        const int64_t most = kMostTiles / ((T + p.tile_n - 1) / p.tile_n) * p.tile_m / 256 * 256;
+        piece = p.Vp < most ? p.Vp : most;
+    }
     if (packs) {
         const int64_t room = (int64_t)((p.off[16] - p.off[15]) / ((size_t)p.Tp * (gradient ? bytes : 0) + (size_t)p.Dp * 2)) / 256 * 256;
         if (piece > room) piece = room;

@@ -54,3 +54,19 @@ def test_a_workspace_for_more_outputs_serves_fewer_at_random_sizes():
         T, D, V = (int(2 ** r.uniform(0, top)) for top in (17, 13, 19))
         loss, dH, dW, both = (L.qless_token_loss_workspace(T, D, V, *want) for want in ((0, 0), (1, 0), (0, 1), (1, 1)))
         assert 0 < loss <= dH <= both and loss <= dW <= both, (T, D, V)
+
+
+def test_more_tokens_than_a_launch_takes_are_refused():
+    """256 threads a token, of fewer than 2^32; tiles of 256 x 256 of dH, of 512 threads."""
+    L = binding.lib()
+
+    def status(T, D, dH, dW):
+        return L.qless_token_loss(one, D, one, D, 1, T, D, 100, one, None, one, None, dH, D, dW, D, None, 0, None)
+    most = (1 << 24) - 256
+    for T, D in ((most + 1, 8), (1 << 24, 64), ((1 << 30) - 1, 8), (1 << 23, 65536), (most, 32769)):
+        for dH, dW in ((None, None), (one, None), (None, one), (one, one)):
+            assert status(T, D, dH, dW) == UNSUPPORTED, (T, D)
+            assert L.qless_token_loss_workspace(T, D, 100, dH is not None, dW is not None) == 0
+    for T, D in ((most, 8), (most, 32000), (1 << 22, 65536)):
+        assert status(T, D, one, None) == WORKSPACE
+        assert L.qless_token_loss_workspace(T, D, 100, 1, 0) > 0
