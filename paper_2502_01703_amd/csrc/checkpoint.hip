@@ -14,6 +14,7 @@
 namespace qless {
 
 constexpr int kGroup = QLESS_CHECKPOINT_GROUP;
+constexpr int64_t kMostThreads = ((int64_t)1 << 32) - 256; // of a launch, in whole workgroups of 256
 
 __device__ inline float bf16_value(uint32_t bits) { return __uint_as_float(bits << 16); }
 __device__ inline uint16_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
@@ -856,7 +857,12 @@ static qless_status launch_grad_rows(const GradArgs &a, hipStream_t st) {
 static bool checkpoint_shape_ok(int64_t T, int32_t D, int64_t ldX, int64_t ldC, int64_t ldS) {
     return T >= 0 && D >= 1 && (T <= 1 || (ldX >= D && ldC >= D && ldS >= (D + (int64_t)kGroup - 1) / kGroup));
 }
-static int64_t checkpoint_grid(int64_t T, int32_t groups) { return (T * groups + kItems - 1) / kItems; }
+// Rows of a launch, and its workgroups.
+static int64_t checkpoint_rows(int64_t T, int32_t groups) {
+    const int64_t most = kMostThreads / 256 * kItems / groups;
+    return T < most ? T : most;
+}
+static unsigned checkpoint_grid(int64_t rows, int32_t groups) { return (unsigned)((rows * groups + kItems - 1) / kItems); }
 
 }  // namespace qless
 
@@ -867,13 +873,18 @@ extern "C" qless_status qless_checkpoint8(const void *X, qless_dtype dt, int64_t
     if (dt != QLESS_F32 && dt != QLESS_BF16) return QLESS_ERR_UNSUPPORTED;
     if (T == 0) return QLESS_OK;
     if (!X || !codes || !step) return QLESS_ERR_INVALID_ARG;
-    const int32_t groups = (D + kGroup - 1) / kGroup;
-    if (T > ((int64_t)1 << 40) / groups || checkpoint_grid(T, groups) > 0x7FFFFFFF) return QLESS_ERR_UNSUPPORTED;
+    const int32_t groups = (int32_t)((D + (int64_t)kGroup - 1) / kGroup);
+    if (T > ((int64_t)1 << 40) / groups) return QLESS_ERR_UNSUPPORTED;
     const hipStream_t st = (hipStream_t)stream;
-    if (dt == QLESS_F32)
-        hipLaunchKernelGGL(checkpoint_write_kernel<float>, dim3((unsigned)checkpoint_grid(T, groups)), dim3(256), 0, st, (const float *)X, T, D, ldX, groups, codes, ldC, step, ldS);
-    else
-        hipLaunchKernelGGL(checkpoint_write_kernel<uint16_t>, dim3((unsigned)checkpoint_grid(T, groups)), dim3(256), 0, st, (const uint16_t *)X, T, D, ldX, groups, codes, ldC, step, ldS);
+    const int64_t rows = checkpoint_rows(T, groups);
+    for (int64_t t = 0; t < T; t += rows) {
+        const int64_t n = T - t < rows ? T - t : rows;
+        auto write = [&](auto kernel, auto *x) {
+            hipLaunchKernelGGL(kernel, dim3(checkpoint_grid(n, groups)), dim3(256), 0, st, x + t * ldX, n, D, ldX, groups, codes + t * ldC, ldC, step + t * ldS, ldS);
+        };
+        if (dt == QLESS_F32) write(checkpoint_write_kernel<float>, (const float *)X);
+        else write(checkpoint_write_kernel<uint16_t>, (const uint16_t *)X);
+    }
     return launch_status();
 }
 
@@ -884,13 +895,18 @@ extern "C" qless_status qless_checkpoint8_read(const int8_t *codes, int64_t ldC,
     if (dt != QLESS_F32 && dt != QLESS_BF16) return QLESS_ERR_UNSUPPORTED;
     if (T == 0) return QLESS_OK;
     if (!X || !codes || !step) return QLESS_ERR_INVALID_ARG;
-    const int32_t groups = (D + kGroup - 1) / kGroup;
-    if (T > ((int64_t)1 << 40) / groups || checkpoint_grid(T, groups) > 0x7FFFFFFF) return QLESS_ERR_UNSUPPORTED;
+    const int32_t groups = (int32_t)((D + (int64_t)kGroup - 1) / kGroup);
+    if (T > ((int64_t)1 << 40) / groups) return QLESS_ERR_UNSUPPORTED;
     const hipStream_t st = (hipStream_t)stream;
-    if (dt == QLESS_F32)
-        hipLaunchKernelGGL(checkpoint_read_kernel<float>, dim3((unsigned)checkpoint_grid(T, groups)), dim3(256), 0, st, codes, ldC, step, ldS, T, D, groups, (float *)X, ldX);
-    else
-        hipLaunchKernelGGL(checkpoint_read_kernel<uint16_t>, dim3((unsigned)checkpoint_grid(T, groups)), dim3(256), 0, st, codes, ldC, step, ldS, T, D, groups, (uint16_t *)X, ldX);
+    const int64_t rows = checkpoint_rows(T, groups);
+    for (int64_t t = 0; t < T; t += rows) {
+        const int64_t n = T - t < rows ? T - t : rows;
+        auto read = [&](auto kernel, auto *x) {
+            hipLaunchKernelGGL(kernel, dim3(checkpoint_grid(n, groups)), dim3(256), 0, st, codes + t * ldC, ldC, step + t * ldS, ldS, n, D, groups, x + t * ldX, ldX);
+        };
+        if (dt == QLESS_F32) read(checkpoint_read_kernel<float>, (float *)X);
+        else read(checkpoint_read_kernel<uint16_t>, (uint16_t *)X);
+    }
     return launch_status();
 }
 
