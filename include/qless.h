@@ -375,7 +375,7 @@ qless_status qless_checkpoint8_read(const int8_t *codes, int64_t ldC, const floa
  *   dY       device, T x R, leading dimension ldY >= R, dtype dtY
  *   codes, step   as written by qless_checkpoint8
  *   offsets  device, n + 1 int64, not decreasing, within [0, T] (others give an unspecified G; nothing outside the operands
- *            is touched);  n <= 65535
+ *            is touched);  n <= 65535;  R, D <= 2^30, ceil(R / 64) ceil(D / 128) < 2^24, T R, T D <= 2^40
  *   G        device, n rows of R * D, leading dimension ldG >= R * D (not read where n == 1), dtype dtG; what lies between the rows stays
  *   ws       device workspace, 16-byte aligned, of at least qless_checkpoint8_grad_workspace(T, n, R, D) bytes
  * Arithmetic: fp32 G: products of dY and step enter whole (dtY bfloat16) or to 2^-24 (fp32), products with codes are exact, sums are fp32.

@@ -179,7 +179,7 @@ struct GradArgs {
     const int8_t *codes; int64_t ldC;
     const float *step; int64_t ldS;
     const int64_t *offsets;
-    int64_t n, T, chunk, segments;
+    int64_t n, T, chunk, segments, first;                  // first: segment of a launch
     int32_t R, D, rtiles, dtiles;
     int32_t Rc, Dc;                                        // columns of dY and codes that may be read: R and D, or more where they are packed
     void *G; int64_t ldG;
@@ -353,7 +353,7 @@ checkpoint_grad_kernel(GradArgs a) {
     const int64_t tiles = (int64_t)a.rtiles * a.dtiles, j = blockIdx.x / tiles;
     const int tile = (int)(blockIdx.x - j * tiles), rt = tile / a.dtiles, g = tile - rt * a.dtiles;
     Segment seg;
-    if (!find_segment(a, j, seg)) return;                  // the whole workgroup
+    if (!find_segment(a, a.first + j, seg)) return;        // the whole workgroup
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wy = wave / WX, wx = wave % WX;
     const int r0 = rt * RT, d0 = g * kGroup, l16 = lane & 15, quad = lane >> 4;
     auto yswizzle = [](int k) { return RT == 64 ? (k >> 1) & 3 : RT == 32 ? (k >> 2) & 1 : 0; };
@@ -502,7 +502,7 @@ checkpoint_grad_ring_kernel(GradArgs a) {
     const int64_t tiles = (int64_t)a.rtiles * a.dtiles, j = blockIdx.x / tiles;
     const int tile = (int)(blockIdx.x - j * tiles), rt = tile / a.dtiles, gt = (tile - rt * a.dtiles) * GROUPS;
     Segment seg;
-    if (!find_segment(a, j, seg)) return;                  // the whole workgroup
+    if (!find_segment(a, a.first + j, seg)) return;        // the whole workgroup
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, quad = lane >> 4;
     const unsigned lds0 = (unsigned)(uintptr_t)((__attribute__((address_space(3))) unsigned char *)smem);
     const int groups = (a.D + kGroup - 1) / kGroup, r0 = rt * RT;
@@ -680,8 +680,11 @@ checkpoint_pack_kernel(const T *in, int64_t ld_in, int64_t rows, int32_t cols, T
 }
 template <class T>
 static void launch_pack(const T *in, int64_t ld_in, int64_t rows, int32_t cols, T *out, int32_t ld, hipStream_t st) {
-    const int64_t chunks = rows * (ld / (16 / (int)sizeof(T)));
-    hipLaunchKernelGGL(checkpoint_pack_kernel<T>, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, st, in, ld_in, rows, cols, out, ld);
+    const int64_t chunks = ld / (16 / (int)sizeof(T)), most = kMostThreads / chunks;
+    for (int64_t r = 0; r < rows; r += most) {
+        const int64_t n = rows - r < most ? rows - r : most;
+        hipLaunchKernelGGL(checkpoint_pack_kernel<T>, dim3((unsigned)((n * chunks + 255) / 256)), dim3(256), 0, st, in + r * ld_in, ld_in, n, cols, out + r * ld, ld);
+    }
 }
 
 // The planes of the examples of more than one segment, added in the order of their tokens.
@@ -757,12 +760,12 @@ static int64_t expand_ld(int32_t D) { return ((int64_t)D + 7) / 8 * 8; }
 static bool many_rows(int64_t T, int64_t n, int32_t R, int32_t D) {
     return R >= 1024 && T >= 128 * n && n * ((R + 255) / 256) * ((D + 255) / 256) >= (n == 1 ? compute_units() / 2 : compute_units());
 }
+static bool expand_fits(int64_t T, int64_t n, int32_t D) { return launchable(n + T / 64, 256) && expand_ld(D) < (1 << 22); }      // (the product's rows of it, too)
 static size_t expand_bytes(int64_t T, int64_t n, int32_t D) { return (size_t)(n + T / 64) * 64 * (size_t)expand_ld(D) * 2; }
 
 static qless_status launch_many(const GradArgs &a, hipStream_t st) {
     uint16_t *x = (uint16_t *)a.planes;
     const int64_t ld = expand_ld(a.D), blocks = a.n + a.T / 64;
-    if (blocks > 0x7FFFFFFF / 64) return QLESS_ERR_UNSUPPORTED;
     const ProductArgs p{ProductOperand{x, ld * 2, ld * 2, blocks * 64}, ProductOperand{a.dY, a.ldY * 2, (int64_t)a.Rc * 2, 0},
                         a.R, a.T, nullptr, nullptr, (a.D + 255) / 256, (int32_t)a.n, a.offsets, nullptr, 0, 0};
     hipLaunchKernelGGL(checkpoint_expand_kernel, dim3((unsigned)blocks, (unsigned)((ld + 127) / 128)), dim3(256), 0, st, a, x, ld);
@@ -817,15 +820,19 @@ static void launch_join(const GradArgs &a, hipStream_t st) {
     if (size % 4 == 0) hipLaunchKernelGGL((checkpoint_join_kernel<Out, 4>), dim3((unsigned)bx, (unsigned)a.n), dim3(256), 0, st, a);
     else hipLaunchKernelGGL((checkpoint_join_kernel<Out, 1>), dim3((unsigned)bx, (unsigned)a.n), dim3(256), 0, st, a);
 }
+// As many segments at a time as a launch takes.
+template <class Out, class Launch>
+static qless_status launch_segments(GradArgs &a, hipStream_t st, Launch launch) {
+    const int64_t tiles = (int64_t)a.rtiles * a.dtiles, most = kMostThreads / 256 / tiles;
+    for (a.first = 0; a.first < a.segments; a.first += most) launch((unsigned)((a.segments - a.first < most ? a.segments - a.first : most) * tiles));
+    launch_join<Out>(a, st);
+    return launch_status();
+}
 template <int RT, class Y, int TERMS, class Out>
 static qless_status launch_grad(GradArgs a, hipStream_t st) {
     a.rtiles = (a.R + RT - 1) / RT;
     a.dtiles = (a.D + kGroup - 1) / kGroup;
-    const int64_t grid = a.segments * a.rtiles * a.dtiles;
-    if (grid > 0x7FFFFFFF) return QLESS_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((checkpoint_grad_kernel<RT, Y, TERMS, Out>), dim3((unsigned)grid), dim3(256), 0, st, a);
-    launch_join<Out>(a, st);
-    return launch_status();
+    return launch_segments<Out>(a, st, [&](unsigned grid) { hipLaunchKernelGGL((checkpoint_grad_kernel<RT, Y, TERMS, Out>), dim3(grid), dim3(256), 0, st, a); });
 }
 template <int RT, class Y, class Out>
 static qless_status launch_ring(GradArgs a, hipStream_t st) {
@@ -833,11 +840,7 @@ static qless_status launch_ring(GradArgs a, hipStream_t st) {
     QLESS_LDS_KERNEL((checkpoint_grad_ring_kernel<RT, Y, Out>), Ring::LDS);
     a.rtiles = (a.R + RT - 1) / RT;
     a.dtiles = (a.D + kGroup * Ring::GROUPS - 1) / (kGroup * Ring::GROUPS);
-    const int64_t grid = a.segments * a.rtiles * a.dtiles;
-    if (grid > 0x7FFFFFFF) return QLESS_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((checkpoint_grad_ring_kernel<RT, Y, Out>), dim3((unsigned)grid), dim3(64 * Ring::NW), Ring::LDS, st, a);
-    launch_join<Out>(a, st);
-    return launch_status();
+    return launch_segments<Out>(a, st, [&](unsigned grid) { hipLaunchKernelGGL((checkpoint_grad_ring_kernel<RT, Y, Out>), dim3(grid), dim3(64 * Ring::NW), Ring::LDS, st, a); });
 }
 template <class Y, class Out>
 static qless_status launch_ring_rows(const GradArgs &a, hipStream_t st) {
@@ -863,6 +866,11 @@ static int64_t checkpoint_rows(int64_t T, int32_t groups) {
     return T < most ? T : most;
 }
 static unsigned checkpoint_grid(int64_t rows, int32_t groups) { return (unsigned)((rows * groups + kItems - 1) / kItems); }
+// The sizes of a gradient: rows and columns that 32 bits count, an example's tiles in a launch, tensors of at most 2^40 numbers.
+static bool grad_sizes_ok(int64_t T, int32_t R, int32_t D) {
+    const int64_t most = (int64_t)1 << 40;
+    return R <= 1 << 30 && D <= 1 << 30 && (int64_t)((R + 63) / 64) * ((D + kGroup - 1) / kGroup) <= kMostThreads / 256 && T <= most / R && T <= most / D;
+}
 
 }  // namespace qless
 
@@ -912,7 +920,7 @@ extern "C" qless_status qless_checkpoint8_read(const int8_t *codes, int64_t ldC,
 
 extern "C" size_t qless_checkpoint8_grad_workspace(int64_t T, int64_t n, int32_t R, int32_t D) {
     using namespace qless;
-    if (T < 0 || n < 1 || R < 1 || D < 1) return 0;
+    if (T < 0 || n < 1 || R < 1 || D < 1 || !grad_sizes_ok(T, R, D)) return 0;
     const int64_t segments = grad_segments(T, n, grad_chunk(T, n, R, D));
     const size_t planes = segments > n ? (size_t)segments * (size_t)R * (size_t)D * 4 : 0, rows = many_rows(T, n, R, D) ? expand_bytes(T, n, D) : 0;
     return up16((planes > rows ? planes : rows)) + packed_bytes(T, n, R, D);
@@ -924,11 +932,11 @@ extern "C" qless_status qless_checkpoint8_grad(const void *dY, qless_dtype dtY, 
     using namespace qless;
     if (R < 1 || n < 0 || !checkpoint_shape_ok(T, D, D, ldC, ldS) || (T > 1 && ldY < R)) return QLESS_ERR_INVALID_ARG;
     if ((dtY != QLESS_F32 && dtY != QLESS_BF16) || (dtG != QLESS_F32 && dtG != QLESS_BF16)) return QLESS_ERR_UNSUPPORTED;
-    if (n > 65535) return QLESS_ERR_UNSUPPORTED;
+    if (n > 65535 || !grad_sizes_ok(T, R, D)) return QLESS_ERR_UNSUPPORTED;
     if (n > 1 && ldG < (int64_t)R * D) return QLESS_ERR_INVALID_ARG;
     if (n == 0) return QLESS_OK;
     if (!offsets || !G || (T > 0 && (!dY || !codes || !step))) return QLESS_ERR_INVALID_ARG;
-    GradArgs a{dY, ldY, codes, ldC, step, ldS, offsets, n, T, grad_chunk(T, n, R, D), 0, R, D, 0, 0, R, D, G, ldG, (float *)ws};
+    GradArgs a{dY, ldY, codes, ldC, step, ldS, offsets, n, T, grad_chunk(T, n, R, D), 0, 0, R, D, 0, 0, R, D, G, ldG, (float *)ws};
     a.segments = grad_segments(T, n, a.chunk);
     const size_t need = qless_checkpoint8_grad_workspace(T, n, R, D);
     if (need > 0 && (!ws || ws_bytes < need || ((uintptr_t)ws & 15) != 0)) return QLESS_ERR_WORKSPACE;
@@ -936,9 +944,9 @@ extern "C" qless_status qless_checkpoint8_grad(const void *dY, qless_dtype dtY, 
     if (ready != QLESS_OK) return ready;
     const hipStream_t st = (hipStream_t)stream;
     const int bytes = dtY == QLESS_BF16 ? 2 : 4, rc = packed_R(R, bytes);
-    if (T > 0 && T <= 0x3FFFFFFF && (int64_t)T * (rc * (int64_t)bytes / 16) < ((int64_t)1 << 38) && (int64_t)T * (packed_D(D) / 16) < ((int64_t)1 << 38)) {
+    if (T > 0 && T <= 0x3FFFFFFF) {
         unsigned char *pack = (unsigned char *)ws + (need - packed_bytes(T, n, R, D));
-        const bool many = dtY == QLESS_BF16 && dtG == QLESS_BF16 && expand_ld(D) < (1 << 22) && many_rows(T, n, R, D);
+        const bool many = dtY == QLESS_BF16 && dtG == QLESS_BF16 && expand_fits(T, n, D) && many_rows(T, n, R, D);
         if (rc != R && worth_packing(T, n, R, D)) {
             if (bytes == 2) launch_pack((const uint16_t *)dY, ldY, T, R, (uint16_t *)pack, rc, st);
             else launch_pack((const float *)dY, ldY, T, R, (float *)pack, rc, st);

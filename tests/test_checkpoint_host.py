@@ -70,3 +70,18 @@ def test_plain_codes_round_to_even():
     X = torch.tensor([[127.0, 0.5, 1.5, 2.5, -0.5, -1.5, 126.5, 0.4999999]])
     codes, steps = plain.checkpoint(X)
     assert steps.item() == 1.0 and codes.tolist() == [[127, 0, 2, 2, 0, -2, 126, 0]]
+
+
+def test_gradient_sizes_that_32_bits_do_not_count_are_refused():
+    """Rows and columns up to 2^30, fewer than 2^24 tiles of an example, tensors of up to 2^40 numbers; what is refused asks for no workspace."""
+    L = binding.lib()
+
+    def status(T, n, R, D):
+        return L.qless_checkpoint8_grad(one, 1, R, R, one, D, one, -(-D // 128), D, T, one, n, one, 0, R * D, None, 0, None)
+    for T, n, R, D in ((1, 1, (1 << 30) + 1, 1), (1, 1, (1 << 31) - 1, 1), (1, 1, 1, (1 << 30) + 1), (1, 1, 1, (1 << 31) - 1), (100, 2, (1 << 31) - 1, (1 << 31) - 1),
+                       (10, 1, 1 << 21, 1 << 20), (1, 1, 1 << 30, 1), (1, 1, 1 << 29, 129), (1 << 30, 1, 1 << 11, 16), (1 << 30, 1, 16, 1 << 11), ((1 << 40) + 1, 1, 1, 1), (1 << 62, 1, 1, 1)):
+        assert status(T, n, R, D) == UNSUPPORTED, (T, n, R, D)
+        assert L.qless_checkpoint8_grad_workspace(T, n, R, D) == 0, (T, n, R, D)
+    for T, n, R, D in ((1 << 40, 1, 1, 1), (1 << 30, 1, 1 << 10, 1 << 10)):
+        assert L.qless_checkpoint8_grad_workspace(T, n, R, D) > 0
+        assert status(T, n, R, D) == WORKSPACE, (T, n, R, D)

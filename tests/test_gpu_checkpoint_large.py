@@ -43,3 +43,30 @@ def test_the_longest_row():
     for a in range(0, D, 1 << 28):
         X[:, a:a + (1 << 28)].normal_(generator=g)
     _whole(X, [(slice(0, 1), slice(a, b)) for a, b in ((0, 12800), ((1 << 30) - 1280, (1 << 30) + 1280), (D - 127 - 1280, D))])
+
+
+def test_more_segments_than_a_launch_takes():
+    """65535 examples, most of them empty, of 300 tiles each."""
+    n, R, D, T = 65535, 1, 38400, 400
+    _say("gradient of %d examples of 300 tiles" % n)
+    g = torch.Generator().manual_seed(3)
+    codes, step = Q.checkpoint8(torch.randn(T, D, generator=g).to(DEV))
+    dY = torch.randn(T, R, generator=g).bfloat16().to(DEV)
+    full = sorted({0, 1, 700, n // 2, 55922, 55923, 55924, n - 2, n - 1})            # a launch takes 55924 of them
+    lengths = torch.zeros(n, dtype=torch.int64)
+    lengths[full] = torch.tensor([T // len(full)] * (len(full) - 1) + [T - T // len(full) * (len(full) - 1)])
+    offsets = torch.cat([torch.zeros(1, dtype=torch.int64), lengths.cumsum(0)])
+    G = torch.full((n, R * D), 7.0, dtype=torch.bfloat16, device=DEV)
+    Q.checkpoint8_grad(dY, codes, step, offsets.to(DEV), out=G)
+    x = codes.double() * step.double().repeat_interleave(Q.CHECKPOINT_GROUP, 1)
+    for e in full:
+        a, b = int(offsets[e]), int(offsets[e + 1])
+        y = dY[a:b].double()
+        ref, size = torch.mm(y.t().contiguous(), x[a:b])[0], torch.mm(y.abs().t().contiguous(), x[a:b].abs())[0]
+        bound = (b - a + 64) * 2.0 ** -23 * size + 2.0 ** -8 * size * (1 + 2.0 ** -8) + 2.0 ** -8 * ref.abs()
+        assert ((G[e].double() - ref).abs() <= bound).all(), e
+    rows = torch.ones(n, dtype=torch.bool)
+    rows[full] = False
+    rows = rows.nonzero()[:, 0].to(DEV)
+    for a in range(0, len(rows), 8192):
+        assert not G[rows[a:a + 8192]].any()
