@@ -936,6 +936,7 @@ extern "C" qless_status qless_checkpoint8_grad(const void *dY, qless_dtype dtY, 
     if (n > 1 && ldG < (int64_t)R * D) return QLESS_ERR_INVALID_ARG;
     if (n == 0) return QLESS_OK;
     if (!offsets || !G || (T > 0 && (!dY || !codes || !step))) return QLESS_ERR_INVALID_ARG;
+    if (T <= 1) { ldY = R; ldC = D; ldS = (D + kGroup - 1) / kGroup; }
     GradArgs a{dY, ldY, codes, ldC, step, ldS, offsets, n, T, grad_chunk(T, n, R, D), 0, 0, R, D, 0, 0, R, D, G, ldG, (float *)ws};
     a.segments = grad_segments(T, n, a.chunk);
     const size_t need = qless_checkpoint8_grad_workspace(T, n, R, D);

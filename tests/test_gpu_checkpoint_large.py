@@ -1,4 +1,4 @@
-"""Checkpoints and gradients of more work items than a launch takes."""
+"""Checkpoints and gradients of more work items than a launch takes, and of rows that only 32-bit products of their sizes would miscount."""
 import pytest
 import torch
 
@@ -70,3 +70,28 @@ def test_more_segments_than_a_launch_takes():
     rows = rows.nonzero()[:, 0].to(DEV)
     for a in range(0, len(rows), 8192):
         assert not G[rows[a:a + 8192]].any()
+
+
+@pytest.mark.parametrize("R,dtype", [((1 << 22) + 8, torch.bfloat16), ((1 << 22) + 5, torch.float32), ((1 << 29) + 64, torch.float32), ((1 << 30) - 64, torch.bfloat16)])
+def test_many_rows_of_one_token(R, dtype):
+    """One token: leading dimensions say nothing of the row's length."""
+    _say("gradient of one token, R=%d %s" % (R, dtype))
+    dY = torch.empty(1, R, device=DEV, dtype=dtype).normal_(generator=torch.Generator(device=DEV).manual_seed(4))
+    codes, step = Q.checkpoint8(torch.tensor([[1.7]], device=DEV))
+    G = Q.checkpoint8_grad(dY, codes, step, torch.tensor([0, 1], device=DEV))
+    x = (codes.double() * step.double()).item()
+    for a in range(0, R, 1 << 26):
+        ref = dY[0, a:a + (1 << 26)].double() * x
+        assert ((G[0, a:a + (1 << 26), 0].double() - ref).abs() <= 65 * 2.0 ** -23 * ref.abs()).all()
+
+
+@pytest.mark.parametrize("D", [(1 << 24) + 16, (1 << 24) + 5])
+def test_many_columns_of_one_token(D):
+    _say("gradient of one token, D=%d" % D)
+    g = torch.Generator(device=DEV).manual_seed(5)
+    codes, step = Q.checkpoint8(torch.randn(1, D, generator=g, device=DEV))
+    dY = torch.randn(1, 8, generator=g, device=DEV).bfloat16()
+    G = Q.checkpoint8_grad(dY, codes, step, torch.tensor([0, 1], device=DEV))
+    x = codes.double() * step.double().repeat_interleave(Q.CHECKPOINT_GROUP, 1)[:, :D]
+    ref = dY.double().t() * x
+    assert ((G[0].double() - ref).abs() <= 65 * 2.0 ** -23 * ref.abs()).all()
