@@ -357,7 +357,8 @@ qless_status qless_token_loss(const void *H, int64_t ldH, const void *W, int64_t
  *   X      device, T x D, row-major with leading dimension ldX (elements) >= D, dtype dt
  *   codes  device, T rows of D int8, leading dimension ldC >= D (bytes between a row's end and the next row are left as they are)
  *   step   device, T rows of ceil(D / QLESS_CHECKPOINT_GROUP) fp32, leading dimension ldS
- * qless_checkpoint8_read writes X = code * step, rounded once (to nearest even) for QLESS_BF16.  No alignment is required of
+ * qless_checkpoint8_read writes X = code * step, rounded once (to nearest even) for QLESS_BF16.  Where 127 steps lie past the largest
+ * bfloat16 (groups that hold one of its largest few numbers), they are read back as it, not as infinity.  No alignment is required of
  * rows beyond that of their elements.  T == 0 is valid; leading dimensions are not read where T <= 1.
  * ------------------------------------------------------------------------------------------- */
 #define QLESS_CHECKPOINT_GROUP 128

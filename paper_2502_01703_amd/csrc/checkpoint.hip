@@ -45,10 +45,14 @@ template <> struct Eight<uint16_t> {                      // bfloat16
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = bf16_value(b[i]);
     }
+    // activations: codes times steps.  127 steps may lie less than one past the largest bfloat16, and stand for it, not for infinity
     static __device__ inline void store(uint16_t *p, int64_t left, const float (&x)[8]) {
         uint16_t b[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) b[i] = bf16_bits(x[i]);
+        for (int i = 0; i < 8; ++i) {
+            b[i] = bf16_bits(x[i]);
+            b[i] -= (b[i] & 0x7FFF) == 0x7F80 ? 1 : 0;
+        }
         if (left >= 8) __builtin_memcpy(p, b, 16);
         else
 #pragma unroll
