@@ -321,8 +321,9 @@ qless_status qless_score_groups(const void *const *train_codes, const float *con
 
 /* ---------------------------------------------------------------------------------------------
  * Loss of a batch of tokens over the vocabulary, with its gradients, from the last hidden states H (a row per token) and the
- * head's weights W (a row per vocabulary entry); the T x V logits are never stored (a piece of the vocabulary at a time passes through
- * the workspace).  With z_t = W H_t:
+ * head's weights W (a row per vocabulary entry).  Of the T x V logits the workspace holds a piece of the vocabulary at a time, all of them only
+ * where they are few: up to 2^22 entries (6 bytes each) for at most 32 tokens, for more 1.5 GB or 2048 entries a token, whichever is more (2 bytes an
+ * entry, 6 where dW is taken in one pass); the loss alone holds none, but fp32 parts of up to 64 MB where T and V are small.  With z_t = W H_t:
  *   lse[t] = log sum_v exp z_tv        nll[t] = lse[t] - z_t,target[t]
  *   L = sum_t weight[t] nll[t]:        dH = dL / dH,  dW = dL / dW
  * A token whose target lies outside [0, V) (-100, say) is left out: nll, lse and its row of dH are 0, it adds nothing to dW, and its row
@@ -337,8 +338,10 @@ qless_status qless_score_groups(const void *const *train_codes, const float *con
  *              refused); want_dH, want_dW: non-zero if dH (dW) is asked for
  * Arithmetic: products of bfloat16 are exact, logits, maxima, sums and losses fp32.  In the gradients a target's entry of
  * weight (softmax - onehot) is fp32, the others are rounded to bfloat16 once (up to 32 tokens: to two bfloat16 terms); sums are fp32 and
- * rounded once.  Results are run-to-run identical.  Rows of W and H
- * need no alignment beyond their elements'; W is read in place where its rows and D are whole 16-byte chunks, else copied piece by piece.
+ * rounded once.  The target's exponential is kept apart from the others', so that nll and 1 - softmax keep their digits for targets that are all
+ * but certain.  Results are run-to-run identical.  Rows of W and H need no alignment beyond their elements'; W is read in place where it begins at
+ * a multiple of 16 bytes, D and ldW are multiples of 8 and ldW < 2^22, else copied piece by piece.  dW orders the tokens by target with T^2 comparisons
+ * (1 ms for 2^16 tokens, 60 ms for 2^19).
  * A row of W outside the largest finite values makes every token's loss NaN or infinite, as the formulas do.
  * ------------------------------------------------------------------------------------------- */
 size_t qless_token_loss_workspace(int64_t T, int32_t D, int32_t V, int want_dH, int want_dW);
@@ -380,8 +383,12 @@ qless_status qless_checkpoint8_read(const int8_t *codes, int64_t ldC, const floa
  *   G        device, n rows of R * D, leading dimension ldG >= R * D (not read where n == 1), dtype dtG; what lies between the rows stays
  *   ws       device workspace, 16-byte aligned, of at least qless_checkpoint8_grad_workspace(T, n, R, D) bytes
  * Arithmetic: fp32 G: products of dY and step enter whole (dtY bfloat16) or to 2^-24 (fp32), products with codes are exact, sums are fp32.
- * bfloat16 G: one factor of a term (an activation, or dY * step) may be rounded to bfloat16 once (dY fp32: to 16 bits or more), sums are fp32 and rounded once.
+ * bfloat16 G: one factor of a term (an activation, or dY * step) may be rounded to bfloat16 once (dY fp32: to 16 bits or more), sums are fp32 and rounded once;
+ * activations are rounded where dY is bfloat16, R >= 1024, and tokens and G are many enough to fill the chip with 256 x 256 tiles.
+ * Products dY * step have to stay below 2^127: for greater ones, and infinite dY, what the formula makes infinite may be NaN, in all columns of the row of G.
  * Results are run-to-run identical.
+ * Rows need no alignment beyond their elements'.  Rows of dY and codes that begin at multiples of 16 bytes (base and leading dimension) take the faster
+ * kernels; where R or D is not such a multiple, large operands are packed into the workspace first.  The workspace serves every dtype.
  * ------------------------------------------------------------------------------------------- */
 size_t qless_checkpoint8_grad_workspace(int64_t T, int64_t n, int32_t R, int32_t D);
 qless_status qless_checkpoint8_grad(const void *dY, qless_dtype dtY, int64_t ldY, int32_t R, const int8_t *codes, int64_t ldC,

@@ -1,15 +1,15 @@
 // qless_token_loss: softmax cross entropy of tokens over a vocabulary, from the last hidden states H and the head's weights W, with
-// its gradients, without the T x V logits.
+// its gradients, a piece of the T x V logits at a time.
 //   z = H W^T,  lse_t = log sum_v exp z_tv,  nll_t = lse_t - z_t,target,  delta_tv = w_t (exp(z_tv - lse_t) - [v = target_t]),
 //   dH = delta W,  dW = delta^T H.
 // Tokens without a target in the vocabulary are left out: the others' rows of H are gathered first (bounded by T on the host, counted
-// on the device), so that a prompt costs no products.
+// on the device), and the products are of these.  (How dH's is cut is planned from T: see LossPlan::splits.)
 //
 // Loss alone: the tiles of logits end with the maximum and the sum of their exponentials, which are joined.
 // dH: a piece of the vocabulary at a time, one pass over it, as with the running softmax of an attention: planes = planes 2^(R_before - R) +
 // p W, dH = w / s planes + w (p_target - 1) W_target at the end.  The tiles end with p = 2^(z log2 e - r), r the whole number above their
 // own maximum, as bfloat16, with the sum of the others' p in fp32; a small kernel finds R, the greatest r of a token so far; and
-// the product with W takes 2^(r - R) off the exponents of its operand, exactly.  So the logits are never in memory, and p is
+// the product with W takes 2^(r - R) off the exponents of its operand, exactly.  So fp32 logits pass through memory only where D is cut in parts, and p is
 // rounded once.  (With fp32 logits in memory and a kernel that turned them into p, 4096 x 4096 x 131072 took 7.9 ms.)
 // dW needs the sums first, and its operand's factors are not of its entries but of its tokens.  Where the whole vocabulary is one piece,
 // its logits are kept until delta is formed from them; else a second pass forms them again.
@@ -44,7 +44,7 @@ struct LossTokens {                        // workspace views, by live token (pa
 };
 struct LossPlan {
     int64_t T, Tp, Dp, Vp, piece, parts;
-    int32_t D, V, tile_n, tile_m, per_part, splits, raw;
+    int32_t D, V, tile_n, tile_m, per_part, splits, raw;   // splits: of dH's product, as fill the chip if all tokens are live (8192 x 4096 x 32000, 90 % masked: 980 us, not 380)
     bool one_pass;                         // dW without a second pass
     size_t off[20], total;
 };
@@ -364,7 +364,8 @@ template <bool FEW> struct LossPlane {
     }
 };
 
-// rows m are columns of dW, columns n vocabulary entries; the targets' entries of delta are added here in fp32
+// rows m are columns of dW, columns n vocabulary entries; the targets' entries of delta are added here in fp32, one token after the other (1 us each where a
+// wavefront's 64 entries are the targets of thousands)
 struct LossHead {
     struct Args {
         uint16_t *dW; int64_t ld, first; int32_t V, D;
@@ -634,7 +635,8 @@ loss_shift_kernel(LossTokens w, int64_t Tp, int64_t parts, int first) {
 }
 
 // The live tokens in the order of target and token, and where each 64 vocabulary entries begin there: 16 threads count what comes before
-// a token (or before 64 entries).  T (T + V / 64) comparisons, next to the 2 T D V operations of the products.
+// a token (or before 64 entries).  T (T + V / 64) comparisons, next to the 2 T D V operations of the products (2048 x 2048 x 50257: 10 of 1400 us; 2^16 tokens
+// 1.1 ms, 2^19 59 ms).
 __global__ void __launch_bounds__(256)
 loss_order_kernel(LossTokens w, int64_t T, int64_t blocks64) {
     const int live = *w.count, sub = threadIdx.x & 15;
